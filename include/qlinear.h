@@ -295,6 +295,100 @@ int ql_quant_act_opt(const void *x, int64_t ldx, int M, int K, int range, int sc
 int ql_quant_weight_opt(const void *w, int N, int K, int bits, int group, int range, int scope,
                         void *wq_canonical, void *scales, void *wq_kernel, void *scratch, void *stream);
 
+/* ---- Paged key/value cache and attention -------------------------------------------------------------------
+ * What lies between the QKV and the O projection of a decoder layer that serves requests: keys and values of all tokens so far,
+ * in pages of a pool that the requests share, and the attention of the new tokens over them.  Textbook definitions; the paper
+ * names none of this.
+ *
+ * Cache: an opaque buffer of ql_kv_cache_bytes, 256-byte aligned, of `pages` pages; a page holds page_size tokens of every
+ * key/value head.  The slot of a token is page * page_size + (position % page_size).  Inside, blocks of 32 tokens of one head
+ * follow each other, [page][head][page_size / 32], in the order in which the matrix instructions take their operands: keys by
+ * token, values transposed (D = head_dim; j counts the last index):
+ *   bits 16  fp16: K [D/16][2][32 tokens][8], channel 16 a + 8 b + j at [a][b][token][j];
+ *                  V [D/32][2][2][32 channels][8], token 16 s + 8 (j / 4) + 4 h + j % 4 at [channel / 32][s][h][channel % 32][j]
+ *   bits 8   int8 codes stored plus 128, one scale per token and head for K and one for V:
+ *                  K [D/32][2][32 tokens][16], channel 32 a + 16 b + j;
+ *                  V [D/32][2][32 channels][16], token 16 (j / 8) + 8 (j % 8 / 4) + 4 h + j % 4 at [channel / 32][h][channel % 32][j];
+ *                  fp32 [4][32 tokens]: scale of K, scale of V, log2 and reciprocal of the scale of V
+ * Quantization (bits 8) as in ql_quant_act_per_token, over the D channels of a token's head: scale = amax / 127,
+ * code = rne(x * (127 / amax)); a vector with amax < 2^-100 has codes 0 (its scale is stored as 2^-31, of no effect).
+ * A token of which a key or a value of some head is infinite or NaN (keys: after the rotation; bits 16: after the rounding to
+ * fp16) is kept as key NaN, value 0 of that head: queries that see it are NaN, others are not touched by it.
+ * The cache need not be cleared: what no token was written to is never used.
+ *
+ * Sizes: head_dim 64, 128 or 256; page_size a power of two from 32 to 1024; heads >= 1; pages >= 1; pages * page_size < 2^31. */
+typedef struct ql_kv_format {
+    int heads;      /* key/value heads */
+    int head_dim;   /* channels of a head */
+    int page_size;  /* tokens of a page */
+    int pages;      /* pages of the pool */
+    int bits;       /* 16 (fp16) or 8 (int8 codes with scales) */
+} ql_kv_format;
+int ql_kv_cache_bytes(const ql_kv_format *format /* host */, size_t *bytes /* host */);
+
+/* One step of the bookkeeping, on the device: request b goes from old_len[b] to want_len[b] tokens.
+ * A request that grows takes pages from the ring of free pages, in the order of the requests; one that shrinks (0: it has ended)
+ * gives its last pages back, behind the ring's end: pages given back in a call are not taken in the same one.
+ *   old_len, want_len  int32 [requests] (negative: 0; old_len beyond columns * page_size counts as that)
+ *   ring               int32 [pages]: the free pages, pool[1] of them from place pool[0] on, modulo pages
+ *   pool, pool_out     int32 [4]: {first place, number of free pages, tokens left without a slot, 0}; pool_out may be pool.
+ *                      pool_out[3] has to hold 0 on entry (every call leaves it so).  At the start: {0, pages, 0, 0}, ring 0, 1, 2, ...
+ *   block_table        int32 [requests][ld_table], columns used: page of tokens c * page_size ... at [b][c]; entries of pages that the
+ *                      call takes are written, all others left as they were
+ *   kv_len             int32 [requests]: tokens that have a page now: want_len, less where the ring or the columns did not suffice (the
+ *                      next call's old_len; may not overlap the inputs)
+ *   cu_new             int32 [requests + 1]: new tokens (want - old where that is positive) of the requests before b; at most max_tokens
+ *   slots, positions   int32 [max_tokens], by new token: its slot (-1: no page, the cache is not written and not read for it) and
+ *                      its position in the request; entries behind cu_new[requests] are left as they were
+ * Limits: requests <= 4096 and requests * columns < 2^31 (QL_ERR_UNSUPPORTED).  Calls that share a pool, ring or table have to follow
+ * each other; requests == 0: cu_new[0] = 0, pool_out = pool. */
+int ql_kv_resize(const int32_t *old_len, const int32_t *want_len, int requests, int page_size, int32_t *ring, int pages,
+                 const int32_t *pool, int32_t *pool_out, int32_t *block_table, int64_t ld_table, int columns, int32_t *kv_len,
+                 int32_t *cu_new, int32_t *slots, int32_t *positions, int max_tokens, void *stream);
+
+/* New tokens into the cache: rotary embedding of queries and keys, keys and values stored.
+ *   q            fp16 [T, q_heads * D], k, v  fp16 [T, heads * D], leading dimensions ldq, ldk, ldv (column ranges of the fused
+ *                projection's output); q NULL: keys and values only (then q_out NULL and q_heads 0)
+ *   cos_sin      fp32 [max_positions, rotary_dim]: cosines of angles 0 .. rotary_dim/2 - 1 of a position, then their sines, or NULL:
+ *                no rotation (rotary_dim 0; then q has to be NULL as well: nothing would be done to it)
+ *                a, b = channels i and i + rotary_dim/2 become a cos_i - b sin_i and b cos_i + a sin_i, each product and each sum one
+ *                fp32 rounding; channels from rotary_dim on stay.  rotary_dim % 16 == 0, <= D
+ *   positions    int32 [T], clamped to the table (may be NULL without rotation)
+ *   slots        int32 [T]; a token whose slot is not in [0, pages * page_size) is not stored (its query is rotated).  A slot that occurs
+ *                twice in a call holds a mixture of the two tokens afterwards
+ *   q_out        fp16 [T, q_heads * D]: rotated queries, each rounded once; may be q itself (same leading dimension), may otherwise
+ *                not overlap the inputs */
+int ql_kv_append(const void *q, int64_t ldq, const void *k, int64_t ldk, const void *v, int64_t ldv, int T, int q_heads,
+                 const float *cos_sin, int rotary_dim, int max_positions, const int32_t *positions, const int32_t *slots,
+                 void *q_out, int64_t ldqo, void *cache, const ql_kv_format *format /* host */, void *stream);
+
+/* Keys and values of given slots as fp16 rows (code * scale rounded once; the inverse of ql_kv_append up to the quantization):
+ * k, v fp16 [T, heads * D], either may be NULL.  Rows of slots outside [0, pages * page_size) are zeros. */
+int ql_kv_read(const void *cache, const ql_kv_format *format /* host */, const int32_t *slots, int T, void *k, int64_t ldk,
+               void *v, int64_t ldv, void *stream);
+
+/* Attention of the requests' new tokens over the cache:
+ *   y[t, h] = sum_j p_j v[j, g] / sum_j p_j,   p_j = exp(scale * q[t, h] . k[j, g]),   g = h / (q_heads / heads)
+ * over the tokens j of t's request that t sees: all j < kv_len; with `causal` those with j <= position of t as well, and with window > 0
+ * position - window < j.  Tokens on pages outside [0, pages) are not seen.  A row that sees nothing is 0.
+ * Scores, maxima, sums and the output are kept in fp32; the p_j, relative to (a bound of) the row's largest, are rounded to fp16 for the
+ * products with v, the int8 codes take part as they are (their scales in fp32).
+ *   q            fp16 [T, q_heads * D], y  fp16 [T, q_heads * D]; y may be q itself (same leading dimension), may otherwise not overlap it
+ *   block_table  int32 [requests][ld_table], `columns` of each used;  cu_new int32 [requests + 1]: rows cu_new[b] .. cu_new[b+1] - 1 are
+ *                the new tokens of request b, which are not decreasing; rows from cu_new[requests] on are left as they were
+ *   ctx_len      int32 [requests]: position of a request's first new token (may be NULL without `causal`)
+ *   kv_len       int32 [requests]: tokens in the cache, the new ones among them (at most columns * page_size count)
+ *   max_new      the most new tokens that a request has, as far as the caller knows it (0: not known): goes into the choice of the
+ *                kernel, never into the result's correctness
+ *   ws           workspace of ql_paged_attention_bytes for the same sizes, 256-byte aligned: partial results of requests whose tokens
+ *                several workgroups share.  One call at a time; nothing in it is kept
+ * q_heads is a multiple of heads; window >= 0, and 0 without causal; scale finite. */
+int ql_paged_attention_bytes(const ql_kv_format *format /* host */, int T, int requests, int q_heads, int max_new, size_t *bytes /* host */);
+int ql_paged_attention(const void *q, int64_t ldq, int T, int q_heads, const void *cache, const ql_kv_format *format /* host */,
+                       const int32_t *block_table, int64_t ld_table, int columns, const int32_t *cu_new, const int32_t *ctx_len,
+                       const int32_t *kv_len, int requests, float scale, int causal, int window, int max_new, void *y, int64_t ldy,
+                       void *ws, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

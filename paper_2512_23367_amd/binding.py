@@ -29,6 +29,7 @@ EXPORTS = [
     "ql_hadamard_block", "ql_smooth_calibrate", "ql_smooth_scales",
     "ql_quant_act_per_token_transformed", "ql_quant_weight_transformed",
     "ql_act_scale_calibrate", "ql_quant_act_opt", "ql_quant_weight_opt",
+    "ql_kv_cache_bytes", "ql_kv_resize", "ql_kv_append", "ql_kv_read", "ql_paged_attention_bytes", "ql_paged_attention",
 ]
 
 QL_RANGE_SYMMETRIC, QL_RANGE_EQ2 = 0, 1
@@ -40,6 +41,12 @@ class QlPlan(ctypes.Structure):
     _fields_ = [("family", ctypes.c_int), ("variant", ctypes.c_int), ("tile_tokens", ctypes.c_int),
                 ("tile_channels", ctypes.c_int), ("splits", ctypes.c_int), ("est_us", ctypes.c_double),
                 ("rest_channels", ctypes.c_int), ("rest_variant", ctypes.c_int)]
+
+
+class QlKvFormat(ctypes.Structure):
+    """Mirror of the C struct ql_kv_format: QlKvFormat(heads=, head_dim=, page_size=, pages=, bits=)."""
+    _fields_ = [("heads", ctypes.c_int), ("head_dim", ctypes.c_int), ("page_size", ctypes.c_int), ("pages", ctypes.c_int),
+                ("bits", ctypes.c_int)]
 
 
 QL_SCOPE_FINE, QL_SCOPE_TENSOR, QL_SCOPE_STATIC = 0, 1, 2
@@ -97,6 +104,12 @@ def lib() -> ctypes.CDLL:
             "ql_act_scale_calibrate": [vp, i64, i, i, i, vp, vp],
             "ql_quant_act_opt": [vp, i64, i, i, i, i, vp, vp, vp, vp, vp, vp],
             "ql_quant_weight_opt": [vp, i, i, i, i, i, i, vp, vp, vp, vp, vp],
+            "ql_kv_cache_bytes": [c.POINTER(QlKvFormat), szp],
+            "ql_kv_resize": [vp, vp, i, i, vp, i, vp, vp, vp, i64, i, vp, vp, vp, vp, i, vp],
+            "ql_kv_append": [vp, i64, vp, i64, vp, i64, i, i, vp, i, i, vp, vp, vp, i64, vp, c.POINTER(QlKvFormat), vp],
+            "ql_kv_read": [vp, c.POINTER(QlKvFormat), vp, i, vp, i64, vp, i64, vp],
+            "ql_paged_attention_bytes": [c.POINTER(QlKvFormat), i, i, i, i, szp],
+            "ql_paged_attention": [vp, i64, i, i, vp, c.POINTER(QlKvFormat), vp, i64, i, vp, vp, vp, i, c.c_float, i, i, i, vp, i64, vp, sz, vp],
         }
         for name, args in sigs.items():
             fn = getattr(l, name)
@@ -422,3 +435,127 @@ def ql_w4a8_gemm_acc_i32(xq_kernel, M, K, w4_kernel, group, N, acc, partials=Non
     wsp, wsb = _ws(ws)
     _check(lib().ql_w4a8_gemm_acc_i32(_p(xq_kernel), M, K, _p(w4_kernel), group, N, _p(acc), _p(partials), row0,
                                       nrows, wsp, wsb, _stream()))
+
+
+# ---- the paged key/value cache and attention over it ----
+
+def _here(*tensors):
+    """All on the device whose stream the call goes to."""
+    at = torch.cuda.current_device() if _current_device is None else _current_device()
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.get_device() != at):
+            raise ValueError("tensors of the current device expected")
+
+
+def _ints(t, name, n):
+    _want(t, torch.int32, name)
+    if t.numel() < n or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous with at least {n} entries")
+    return t.data_ptr()
+
+
+def _heads_of(t, name, rows, head_dim):
+    """Heads in the columns of fp16 [rows, heads * head_dim] with unit inner stride."""
+    _want(t, torch.float16, name)
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] % head_dim or (t.numel() and t.stride(1) != 1):
+        raise ValueError(f"{name} must be [{rows}, heads * {head_dim}] with unit inner stride")
+    return t.shape[1] // head_dim
+
+
+def _row_stride(t):
+    """The leading dimension of a checked matrix (torch gives a single row any stride: its columns do as well)."""
+    return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else (t.shape[1] + 7) // 8 * 8
+
+
+def _kv_rows(t, name, rows, fmt):
+    if _heads_of(t, name, rows, fmt.head_dim) != fmt.heads:
+        raise ValueError(f"{name} must have the cache's {fmt.heads} heads of {fmt.head_dim}")
+
+
+@functools.lru_cache(maxsize=256)
+def _cache_bytes(*sizes) -> int:
+    a = ctypes.c_size_t()
+    _check(lib().ql_kv_cache_bytes(ctypes.byref(QlKvFormat(*sizes)), ctypes.byref(a)))
+    return a.value
+
+
+def ql_kv_cache_bytes(fmt: QlKvFormat) -> int:
+    return _cache_bytes(fmt.heads, fmt.head_dim, fmt.page_size, fmt.pages, fmt.bits)
+
+
+def _cache(cache, fmt):
+    if not cache.is_contiguous() or cache.nbytes < ql_kv_cache_bytes(fmt):
+        raise ValueError("cache must be contiguous with at least the bytes of ql_kv_cache_bytes")
+    return cache.data_ptr()
+
+
+def _table(t, requests):
+    _want(t, torch.int32, "block_table")
+    if t.dim() != 2 or t.shape[0] < requests or (t.numel() and t.stride(1) != 1):
+        raise ValueError(f"block_table must be [{requests}, columns] with unit inner stride")
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])), t.shape[1]
+
+
+def ql_kv_resize(page_size, old_len, want_len, ring, pool, pool_out, block_table, kv_len, cu_new, slots, positions):
+    """Pages, slots and positions for requests that go from old_len to want_len tokens; all int32 tensors on the device.
+    The pool has ring.numel() pages; slots and positions have room for the step's new tokens."""
+    _here(old_len, want_len, ring, pool, pool_out, block_table, kv_len, cu_new, slots, positions)
+    n, most = old_len.numel(), min(slots.numel(), positions.numel())
+    table, ld, columns = _table(block_table, n)
+    _check(lib().ql_kv_resize(_ints(old_len, "old_len", n), _ints(want_len, "want_len", n), n, page_size, _ints(ring, "ring", 1), ring.numel(),
+                              _ints(pool, "pool", 4), _ints(pool_out, "pool_out", 4), table, ld, columns, _ints(kv_len, "kv_len", n),
+                              _ints(cu_new, "cu_new", n + 1), _ints(slots, "slots", most), _ints(positions, "positions", most), most, _stream()))
+
+
+def ql_kv_append(q, k, v, cos_sin, positions, slots, q_out, cache, fmt):
+    """Rotates q (into q_out, which may be q) and k by cos_sin (fp32 [positions, rotary_dim], or None) and stores k and v."""
+    _here(q, k, v, cos_sin, positions, slots, q_out, cache)
+    T = k.shape[0]
+    _kv_rows(k, "k", T, fmt), _kv_rows(v, "v", T, fmt)
+    q_heads = rotary = most = 0
+    if cos_sin is not None:
+        _want(cos_sin, torch.float32, "cos_sin")
+        if cos_sin.dim() != 2 or not cos_sin.is_contiguous():
+            raise ValueError("cos_sin must be a contiguous [positions, rotary_dim]")
+        most, rotary = cos_sin.shape
+        _ints(positions, "positions", T)
+    if q is not None:
+        q_heads = _heads_of(q, "q", T, fmt.head_dim)
+        if q_out is None or q_out.shape != q.shape or _heads_of(q_out, "q_out", T, fmt.head_dim) != q_heads:
+            raise ValueError("q_out must have q's shape")
+    _check(lib().ql_kv_append(_p(q), _row_stride(q) if q is not None else 0, k.data_ptr(), _row_stride(k), v.data_ptr(), _row_stride(v), T, q_heads,
+                              _p(cos_sin), rotary, most, _p(positions), _ints(slots, "slots", T), _p(q_out),
+                              _row_stride(q_out) if q_out is not None else 0, _cache(cache, fmt), ctypes.byref(fmt), _stream()))
+
+
+def ql_kv_read(cache, fmt, slots, k=None, v=None):
+    """Keys and values of the given slots as fp16 [T, heads * head_dim] (either may be None)."""
+    _here(cache, slots, k, v)
+    T = (k if k is not None else v if v is not None else slots).shape[0]
+    for t, name in ((k, "k"), (v, "v")):
+        if t is not None:
+            _kv_rows(t, name, T, fmt)
+    _check(lib().ql_kv_read(_cache(cache, fmt), ctypes.byref(fmt), _ints(slots, "slots", T), T, _p(k), _row_stride(k) if k is not None else 0,
+                            _p(v), _row_stride(v) if v is not None else 0, _stream()))
+
+
+def ql_paged_attention_bytes(fmt: QlKvFormat, T: int, requests: int, q_heads: int, max_new: int = 0) -> int:
+    a = ctypes.c_size_t()
+    _check(lib().ql_paged_attention_bytes(ctypes.byref(fmt), T, requests, q_heads, max_new, ctypes.byref(a)))
+    return a.value
+
+
+def ql_paged_attention(q, cache, fmt, block_table, cu_new, ctx_len, kv_len, scale, y, ws=None, causal=True, window=0, max_new=0):
+    """Attention of the new tokens q (rows cu_new[b] .. of request b) over the cache; ws: ql_paged_attention_bytes of the same sizes."""
+    _here(q, cache, block_table, cu_new, ctx_len, kv_len, y, ws)
+    T, n = q.shape[0], kv_len.numel()
+    q_heads = _heads_of(q, "q", T, fmt.head_dim)
+    if y.shape != q.shape or _heads_of(y, "y", T, fmt.head_dim) != q_heads:
+        raise ValueError("y must have q's shape")
+    if ctx_len is not None:
+        _ints(ctx_len, "ctx_len", n)
+    table, ld, columns = _table(block_table, n)
+    wsp, wsb = _ws(ws)
+    _check(lib().ql_paged_attention(q.data_ptr(), _row_stride(q), T, q_heads, _cache(cache, fmt), ctypes.byref(fmt), table, ld, columns,
+                                    _ints(cu_new, "cu_new", n + 1), _p(ctx_len), _ints(kv_len, "kv_len", n), n, float(scale), int(causal), window,
+                                    max_new, y.data_ptr(), _row_stride(y), wsp, wsb, _stream()))
