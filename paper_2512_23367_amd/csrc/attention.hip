@@ -1,105 +1,101 @@
-// Attention of new tokens over the paged key/value cache (include/qlinear.h).
-#include "kv_cache.h"
+// Attention over the paged cache: which kernel takes a call, and the sum of partial results (include/qlinear.h).
+#include <cmath>
+
+#include "attention.h"
 
 namespace ql {
 namespace {
 
-typedef _Float16 h8 __attribute__((ext_vector_type(8)));
-typedef unsigned char u8x16 __attribute__((ext_vector_type(16)));
-
-// One wavefront per new token and query head, one pass over the cache in steps of two blocks: lane l scores token l of the
-// step (its key is 16-byte pieces, 512 bytes apart), the running maximum and sum are those of the whole wavefront, and for the output lane l
-// holds channels l, l + 64, ... (whose values of consecutive tokens are 16-byte pieces as well).
-template <int ELEM, int D>
-__global__ __launch_bounds__(64) void attention_kernel(AttnArgs a)
+// Joins the parts of the rows whose tokens several workgroups shared: one workgroup per new token, a wavefront per query head in turn.
+template <int D>
+__global__ __launch_bounds__(ATTN_THREADS) void attn_join_kernel(AttnArgs a, AttnPlan plan)
 {
     constexpr int N = D / 64;
-    __shared__ float sq[D], sp[64], sv[64];
-    const int lane = threadIdx.x, t = blockIdx.x, head = blockIdx.y, g = head / a.group;
-    if (t < a.cu[0] || t >= a.cu[a.requests]) return;
-    int b = 0, hi = a.requests;
-    while (hi - b > 1) {
-        const int mid = (b + hi) / 2;
-        if (a.cu[mid] <= t) b = mid; else hi = mid;
-    }
-    const int len = (int)min((int64_t)max(a.len[b], 0), (int64_t)a.columns << a.kv.page_shift);
-    int first = 0, end = len;
-    if (a.causal) {
-        const int64_t pos = (int64_t)a.ctx[b] + (t - a.cu[b]);
-        end = (int)max((int64_t)0, min((int64_t)len, pos + 1));
-        if (a.window) first = (int)max((int64_t)0, pos - a.window + 1);
-    }
-    for (int i = 0; i < N; ++i) sq[lane + 64 * i] = __half2float(a.q[t * a.ldq + (int64_t)head * D + lane + 64 * i]);
+    __shared__ AttnScratch scratch;
+    __shared__ int owner;
+    const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int64_t tiles;
+    const int64_t work = attn_work<ATTN_THREADS>(a, plan.bm, scratch.part, tiles);
+    const int c = attn_part_units(work, plan.target);
+    // t's request, and the items before it
+    if (tid == 0) owner = -1;
     __syncthreads();
-    float m = -INFINITY, l = 0, o[N];
-    for (int i = 0; i < N; ++i) o[i] = 0;
-    for (int j0 = first & ~63; j0 < end; j0 += 64) {
-        const int j = j0 + lane;
-        auto page_of = [&](int j) { return a.table[b * a.ld_table + (j >> a.kv.page_shift)]; };
-        bool seen = j >= first && j < end;
-        const int page = seen ? page_of(j) : 0;
-        seen = seen && (unsigned)page < (unsigned)a.kv.pages;
-        float s = 0, scale_v = 1;
-        if (seen) {
-            const char *block = a.kv.block(page, g, j & (a.kv.page_size() - 1));
-            const float *of = reinterpret_cast<const float *>(block + kv_scale_offset(D));
-            for (int c = 0; c < D; c += 8) {
-                const char *p = block + kv_key_offset<ELEM>(j % KV_BLOCK, c);
-                for (int i = 0; i < 8; ++i)
-                    s = fmaf(sq[c + i], ELEM == 2 ? __half2float(reinterpret_cast<const __half *>(p)[i]) : (float)(reinterpret_cast<const uint8_t *>(p)[i] - 128), s);
-            }
-            if (ELEM == 1) s *= of[j % KV_BLOCK], scale_v = of[KV_BLOCK + j % KV_BLOCK];
-            s *= a.scale;
-        } else {
-            s = -INFINITY;
-        }
-        float top = s;
-        for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-        const float m_new = fmaxf(m, top), base = m_new == -INFINITY ? 0.f : m_new;
-        const float p = expf(s - base), keep = expf(m - base);
-        float sum = p;
-        for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-        l = l * keep + sum, m = m_new;
-        sp[lane] = p, sv[lane] = seen ? scale_v : 0.f;
-        __syncthreads();
-        for (int i = 0; i < N; ++i) o[i] *= keep;
-        for (int half = 0; half < 64; half += KV_BLOCK) {
-            if (j0 + half >= end || j0 + half + KV_BLOCK <= first) continue;
-            const int pg = page_of(j0 + half);
-            if ((unsigned)pg >= (unsigned)a.kv.pages) continue;
-            const char *block = a.kv.block(pg, g, (j0 + half) & (a.kv.page_size() - 1));
-            for (int i = 0; i < N; ++i)
-                for (int r = 0; r < KV_BLOCK; ++r) {
-                    const char *p = block + kv_value_offset<ELEM>(r, lane + 64 * i, D);
-                    const float x = ELEM == 2 ? __half2float(*reinterpret_cast<const __half *>(p)) : (float)(*reinterpret_cast<const uint8_t *>(p) - 128);
-                    const float w = sv[half + r];
-                    if (w != 0.f) o[i] = fmaf(sp[half + r], x * w, o[i]);
-                }
-        }
-        __syncthreads();
+    for (int b = tid; b < a.requests; b += ATTN_THREADS) {
+        const AttnSpan r = attn_span(a, b);
+        if (t >= r.cu && t < r.cu + r.rows / a.group) owner = b;
     }
-    for (int i = 0; i < N; ++i)
-        a.y[t * a.ldy + (int64_t)head * D + lane + 64 * i] = __float2half(l == 0 ? 0.f : o[i] / l);
+    __syncthreads();
+    const int b = owner;
+    if (b < 0) return;
+    const AttnSpan r = attn_span(a, b);
+    const int parts = attn_parts(r, c);
+    if (parts == 1) return;
+    int64_t n = 0, before;
+    for (int i = tid; i < b; i += ATTN_THREADS) {
+        const AttnSpan s = attn_span(a, i);
+        n += (int64_t)attn_tiles(s, plan.bm) * attn_parts(s, c);
+    }
+    block_sum_before<ATTN_THREADS>(n, scratch.part, before);
+
+    const size_t size = attn_partial_floats(plan.bm, D);
+    for (int head = wave; head < a.q_heads; head += ATTN_THREADS / 64) {
+        const int kvh = head / a.group, row = (t - r.cu) * a.group + head % a.group;
+        const int64_t item = before + (int64_t)(row / plan.bm) * parts;
+        if (item + parts > plan.items) continue;             // (lengths that contradict each other)
+        const float *p0 = static_cast<const float *>(a.ws) + ((size_t)item * a.kv.heads + kvh) * size;
+        const size_t step = (size_t)a.kv.heads * size;
+        const int at = row % plan.bm;
+        float m = -INFINITY;
+        for (int k = 0; k < parts; ++k) m = fmaxf(m, p0[k * step + (size_t)plan.bm * D + at]);
+        float l = 0, o[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) o[i] = 0;
+        for (int k = 0; k < parts; ++k) {
+            const float *p = p0 + k * step;
+            const float mk = p[(size_t)plan.bm * D + at], lk = p[(size_t)plan.bm * (D + 1) + at];
+            const float w = lk == 0.f ? 0.f : __builtin_amdgcn_exp2f(mk - m);
+            l += lk * w;
+#pragma unroll
+            for (int i = 0; i < N; ++i) o[i] = fmaf(lk == 0.f ? 0.f : p[(size_t)at * D + lane + 64 * i], w, o[i]);
+        }
+        const float inv = l == 0.f ? 0.f : 1.0f / l;
+#pragma unroll
+        for (int i = 0; i < N; ++i) a.y[(int64_t)t * a.ldy + (int64_t)head * D + lane + 64 * i] = __float2half(o[i] * inv);
+    }
 }
 
 }  // namespace
 
-size_t attention_workspace_bytes(const KvView &, int, int, int, int) { return 0; }
+AttnPlan attention_plan(const KvView &kv, int T, int requests, int q_heads, int max_new)
+{
+    AttnPlan p = {};
+    const int group = q_heads / kv.heads;
+    p.bm = 128;
+    const int64_t tiles = (int64_t)T * group / p.bm + requests;
+    p.target = tiles * kv.heads >= 512 ? 0 : ceil_div(512, kv.heads);
+    p.items = (int)(tiles + p.target);
+    p.ws_bytes = p.target ? (size_t)p.items * kv.heads * attn_partial_floats(p.bm, kv.D) * 4 : 0;
+    return p;
+}
+
+size_t attention_workspace_bytes(const KvView &kv, int T, int requests, int q_heads, int max_new)
+{
+    return attention_plan(kv, T, requests, q_heads, max_new).ws_bytes;
+}
 
 int launch_attention(const AttnArgs &a, hipStream_t st)
 {
-    const dim3 grid(a.T, a.q_heads);
-    auto run = [&](auto kernel) { kernel<<<grid, 64, 0, st>>>(a); };
-    if (a.kv.bits == 16) {
-        if (a.kv.D == 64) run(attention_kernel<2, 64>);
-        else if (a.kv.D == 128) run(attention_kernel<2, 128>);
-        else run(attention_kernel<2, 256>);
-    } else {
-        if (a.kv.D == 64) run(attention_kernel<1, 64>);
-        else if (a.kv.D == 128) run(attention_kernel<1, 128>);
-        else run(attention_kernel<1, 256>);
-    }
-    return check_hip(hipGetLastError(), "attention_kernel");
+    const AttnPlan p = attention_plan(a.kv, a.T, a.requests, a.q_heads, a.max_new);
+    if ((int64_t)p.items * a.kv.heads >= (int64_t)1 << 31)
+        return fail(QL_ERR_UNSUPPORTED, "%d tokens of %d query heads are more than a launch holds", a.T, a.q_heads);
+    // exp(scale s) = exp2(c s); a scale of nothing keeps masked scores apart from the others (-inf times 0 would be NaN)
+    const float c = fmaxf(std::fabs(a.scale) * 1.44269504088896341f, 1e-30f);
+    QL_TRY(launch_attention_tiles(a, p, c, st));
+    if (!p.target) return QL_OK;
+    if (a.kv.D == 64) attn_join_kernel<64><<<a.T, ATTN_THREADS, 0, st>>>(a, p);
+    else if (a.kv.D == 128) attn_join_kernel<128><<<a.T, ATTN_THREADS, 0, st>>>(a, p);
+    else attn_join_kernel<256><<<a.T, ATTN_THREADS, 0, st>>>(a, p);
+    return check_hip(hipGetLastError(), "attn_join_kernel");
 }
 
 }  // namespace ql

@@ -1,0 +1,327 @@
+// Attention of many new tokens over the paged cache: workgroups of several wavefronts, 32 rows each, that share tiles of keys and values
+// in LDS.
+#include "attention.h"
+#include "gemm_tiles.h"
+#include "quant_math.h"
+
+namespace ql {
+namespace {
+
+__device__ inline unsigned pack2(float a, float b) { return __builtin_bit_cast(unsigned, h2{(_Float16)a, (_Float16)b}); }
+__device__ inline h8 as_h8(u4 v) { return __builtin_bit_cast(h8, v); }
+
+// Four codes (stored plus 128) -> four fp16, exactly: a byte under the exponent of 1024 is 1024 + byte.
+__device__ inline void widen_codes(unsigned w, unsigned &lo, unsigned &hi)
+{
+    const h2 off = {(_Float16)1152, (_Float16)1152};
+    lo = __builtin_bit_cast(unsigned, __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, w, 0x04010400u)) - off);
+    hi = __builtin_bit_cast(unsigned, __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, w, 0x04030402u)) - off);
+}
+
+template <int ELEM, int D, int NW>
+__global__ __launch_bounds__(NW * 64, D == 256 ? 1 : 2) void attn_tile_kernel(AttnArgs a, AttnPlan plan, float c, unsigned flip)
+{
+    constexpr int BM = 32 * NW, TB = D == 256 ? 1 : 2;               // rows; blocks of 32 tokens in a tile of keys
+    constexpr int TOK = 32 * TB, KS = D / 16, ET = D / 32;
+    constexpr int BLOCK = 32 * D * 4;                                // bytes of a block's keys and values in LDS (fp16)
+    constexpr int SC = ELEM == 1 ? 3 * TOK : 1;
+    extern __shared__ __attribute__((aligned(1024))) char stage[];
+    auto tile = [&](int i) { return stage + i * TB * BLOCK; };
+    __shared__ __attribute__((aligned(16))) float scales[2][SC];
+    __shared__ AttnScratch scratch;
+
+    const int kvh = blockIdx.x % a.kv.heads, index = blockIdx.x / a.kv.heads;
+    AttnItem it;
+    if (!attn_item<NW * 64>(a, BM, plan.target, index, scratch, it)) return;
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, h = lane >> 5;
+    const int row0 = it.tile * BM, wrow0 = row0 + wave * 32, row = wrow0 + col;
+    const bool live = row < it.r.rows;
+    const int token = live ? row / a.group : 0, head = kvh * a.group + (live ? row % a.group : 0);
+    // positions: of this lane's row, of the wavefront's first and last
+    auto position = [&](int r) { return (int)min(max((int64_t)it.r.ctx + r / a.group, (int64_t)-1), (int64_t)INT32_MAX); };
+    const int pos = position(live ? row : 0), pos0 = position(wrow0), pos1 = position(min(wrow0 + 32, it.r.rows) - 1);
+
+    int low, high;
+    attn_range(a, it.r, row0, min(row0 + BM, it.r.rows), low, high);
+    attn_part_range(low, high, it.part, it.parts);
+    low = __builtin_amdgcn_readfirstlane(low), high = __builtin_amdgcn_readfirstlane(high);
+
+    // queries: column operand, 8 channels of a step per lane, in the order of the keys' channels
+    h8 q[KS];
+    {
+        const __half *src = a.q + (int64_t)(it.r.cu + token) * a.ldq + (int64_t)head * D;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            const int d = ELEM == 2 ? 16 * s + 8 * h : 32 * (s / 2) + 16 * h + 8 * (s % 2);
+            u4 v = {0, 0, 0, 0};
+            if (live) v = *reinterpret_cast<const u4 *>(src + d);
+            q[s] = as_h8(v ^ flip);
+        }
+    }
+
+    f16v o[ET];
+#pragma unroll
+    for (int e = 0; e < ET; ++e)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[e][i] = 0;
+    float m = -INFINITY, l = 0;
+
+    const int32_t *row_of_table = a.table + (int64_t)it.b * a.ld_table;
+    auto entry = [&](int t) { return row_of_table[t < high ? t >> a.kv.page_shift : 0]; };
+    auto page_of = [&](int entry, int t) {                           // page of token t, -1: none
+        const int p = __builtin_amdgcn_readfirstlane(entry);
+        return t < high && (unsigned)p < (unsigned)a.kv.pages ? p : -1;
+    };
+    auto block_at = [&](int page, int t) { return a.kv.block(max(page, 0), kvh, t & (a.kv.page_size() - 1)); };
+
+    int pages[TB], next[TB], ahead[TB];                              // of the tile at hand, of the next one; table entries of the one after it
+
+    // ---- a tile into LDS ----
+    constexpr int PIECES = ELEM == 2 ? TB * BLOCK / 1024 / NW : TB * BLOCK / 2 / 1024 / NW;   // KB per wavefront, as stored
+    u4 staged[ELEM == 1 ? PIECES : 1];
+    float staged_scale[3];
+    auto fetch = [&](int t, char *to, const int (&pg)[TB]) {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            constexpr int PER = BLOCK / (ELEM == 2 ? 1024 : 2048);   // pieces of a block
+            const int p = i * NW + wave, blk = p / PER, off = p % PER * 1024;
+            // (a block without a page: a buffer of no bytes, whose loads return zeros)
+            const int page = TB == 1 ? pg[0] : blk ? pg[TB - 1] : pg[0];
+            const __amdgpu_buffer_rsrc_t rs = make_rsrc(block_at(page, t + 32 * blk), page >= 0 ? (unsigned)a.kv.block_bytes : 0u);
+            if constexpr (ELEM == 2)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, LDS_PTR(to + p * 1024), 16, off + lane * 16, 0, 0, 0);
+            else
+                staged[i] = __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(rs, off + lane * 16, 0, 0));
+        }
+        if constexpr (ELEM == 1) {
+            if (tid < TOK) {
+                const int blk = tid / 32, page = TB == 1 ? pg[0] : blk ? pg[TB - 1] : pg[0];
+                const float *s = reinterpret_cast<const float *>(block_at(page, t + 32 * blk) + kv_scale_offset(D)) + tid % 32;
+                staged_scale[0] = s[0], staged_scale[1] = s[64], staged_scale[2] = s[96];
+            }
+        }
+    };
+    auto settle = [&](char *to, float *sc) {                         // int8: widen what was fetched into LDS
+        if constexpr (ELEM == 1) {
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                const int p = i * NW + wave;
+                u4 lo, hi;
+                unsigned x, y;
+                widen_codes(staged[i][0], x, y), lo[0] = x, lo[1] = y;
+                widen_codes(staged[i][1], x, y), lo[2] = x, lo[3] = y;
+                widen_codes(staged[i][2], x, y), hi[0] = x, hi[1] = y;
+                widen_codes(staged[i][3], x, y), hi[2] = x, hi[3] = y;
+                *reinterpret_cast<u4 *>(to + p * 2048 + lane * 16) = lo;
+                *reinterpret_cast<u4 *>(to + p * 2048 + 1024 + lane * 16) = hi;
+            }
+            if (tid < TOK) sc[tid] = staged_scale[0] * c, sc[TOK + tid] = staged_scale[1], sc[2 * TOK + tid] = staged_scale[2];
+        } else {
+            wait_vmcnt<0>();
+        }
+    };
+
+    // What lies behind the last token, or on no page, is whatever memory held: its weights are 0, but 0 times NaN is not.  fp16: values of
+    // such tokens are cleared (one tile of a workgroup); int8: the reciprocal scales, codes are finite.
+    auto whole = [&](int t, const int (&pg)[TB]) {
+        bool w = t + TOK <= high;
+#pragma unroll
+        for (int i = 0; i < TB; ++i) w = w && pg[i] >= 0;
+        return w;
+    };
+    auto clear = [&](int t, char *to, float *sc, const int (&pg)[TB]) {
+        if constexpr (ELEM == 1) {
+            if (tid < TOK && !(t + tid < high && (TB == 1 || tid < 32 ? pg[0] : pg[TB - 1]) >= 0)) sc[tid] = 0, sc[TOK + tid] = 0, sc[2 * TOK + tid] = 0;
+        } else {
+            for (int i = tid; i < TB * 2 * ET * 64; i += NW * 64) {  // 8 tokens of a channel each
+                const int blk = i / (2 * ET * 64), at = i % (2 * ET * 64), k = at / 64 % 2, hh = at / 32 % 2;
+                u4 *p = reinterpret_cast<u4 *>(to + blk * BLOCK + 32 * D * 2 + at * 16);
+                u4 v = *p;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int tk = t + 32 * blk + 16 * k + 8 * (e / 4) + 4 * hh + e % 4;
+                    if (!(tk < high && (blk ? pg[TB - 1] : pg[0]) >= 0)) v[e / 2] &= e % 2 ? 0x0000ffffu : 0xffff0000u;
+                }
+                *p = v;
+            }
+        }
+        __syncthreads();
+    };
+
+    // ---- one tile: S^T = K Q^T, softmax down the columns, O^T += V^T P^T ----
+    auto take = [&](bool masked, int t, const char *from, const float *sc, const int (&pg)[TB]) {
+        f16v s[TB];
+#pragma unroll
+        for (int b = 0; b < TB; ++b) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[b][i] = 0;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                const h8 x = *reinterpret_cast<const h8 *>(from + b * BLOCK + k * 1024 + lane * 16);
+                s[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, q[k], s[b], 0, 0, 0);
+            }
+        }
+        if constexpr (ELEM == 1) {
+#pragma unroll
+            for (int b = 0; b < TB; ++b)
+#pragma unroll
+                for (int i4 = 0; i4 < 4; ++i4) {
+                    const int j = 32 * b + 8 * i4 + 4 * h;           // token of the tile of element 4 i4
+                    const f4 sk = *reinterpret_cast<const f4 *>(sc + j), lv = *reinterpret_cast<const f4 *>(sc + TOK + j);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[b][4 * i4 + i] = fmaf(s[b][4 * i4 + i], sk[i], lv[i]);
+                }
+        }
+        if (masked) {
+            asm volatile("");                                        // or the compiler compares and selects for every tile
+#pragma unroll
+            for (int b = 0; b < TB; ++b) {
+                const int last = pg[b] < 0 ? -1 : a.causal ? min(high - 1, pos) : high - 1, first = a.window ? pos - a.window : -1;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int tk = t + 32 * b + 8 * (i / 4) + 4 * h + i % 4;
+                    if (tk > last || tk <= first) s[b][i] = -INFINITY;
+                }
+            }
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int b = 0; b < TB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
+        {
+            unsigned x, y;
+            lane_pair<32>(__builtin_bit_cast(unsigned, top), x, y);
+            top = fmaxf(__builtin_bit_cast(float, x), __builtin_bit_cast(float, y));
+        }
+        constexpr bool RAW = ELEM == 2;                              // scores still without the factor c
+        const float factor = RAW ? c : 1.0f;
+        // The maximum follows only when a score exceeds it by 2^8: weights up to 256 lose nothing in fp16, and the sums are rarely rescaled.
+        if (__any((top - m) * factor > 8.0f)) {
+            const float to = fmaxf(m, top), keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - to) * factor);
+            m = to;
+            l *= keep;
+#pragma unroll
+            for (int e = 0; e < ET; ++e)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[e][i] *= keep;
+        }
+        const float base = m == -INFINITY ? 0.f : -m * factor;
+        h8 p[TB][2];
+#pragma unroll
+        for (int b = 0; b < TB; ++b) {
+            unsigned w[8];
+#pragma unroll
+            for (int i4 = 0; i4 < 4; ++i4) {
+                float x[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = __builtin_amdgcn_exp2f(RAW ? fmaf(s[b][4 * i4 + i], c, base) : s[b][4 * i4 + i] + base);
+                if constexpr (ELEM == 1) {
+                    const f4 iv = *reinterpret_cast<const f4 *>(sc + 2 * TOK + 32 * b + 8 * i4 + 4 * h);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) l = fmaf(x[i], iv[i], l);
+                } else {
+                    l += (x[0] + x[1]) + (x[2] + x[3]);
+                }
+                w[2 * i4] = pack2(x[0], x[1]), w[2 * i4 + 1] = pack2(x[2], x[3]);
+            }
+            p[b][0] = as_h8(u4{w[0], w[1], w[2], w[3]}), p[b][1] = as_h8(u4{w[4], w[5], w[6], w[7]});
+        }
+#pragma unroll
+        for (int b = 0; b < TB; ++b)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+#pragma unroll
+                for (int e = 0; e < ET; ++e) {
+                    const h8 x = *reinterpret_cast<const h8 *>(from + b * BLOCK + 32 * D * 2 + e * 2048 + k * 1024 + lane * 16);
+                    o[e] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, p[b][k], o[e], 0, 0, 0);
+                }
+            }
+    };
+
+    // ---- over the tiles ----
+    if (low < high) {
+#pragma unroll
+        for (int i = 0; i < TB; ++i) next[i] = page_of(entry(low + 32 * i), low + 32 * i), ahead[i] = entry(low + TOK + 32 * i);
+        fetch(low, tile(0), next);
+        settle(tile(0), scales[0]);
+        int cur = 0;
+        for (int t = low; t < high; t += TOK, cur ^= 1) {
+            __syncthreads();                                         // tile t is there, the other buffer is free
+#pragma unroll
+            for (int i = 0; i < TB; ++i)
+                pages[i] = next[i], next[i] = page_of(ahead[i], t + TOK + 32 * i), ahead[i] = entry(t + 2 * TOK + 32 * i);
+            const bool more = t + TOK < high;
+            if (more) fetch(t + TOK, tile(cur ^ 1), next);
+            if (!whole(t, pages)) clear(t, tile(cur), scales[cur], pages);
+            const bool some = wrow0 < it.r.rows && (!a.causal || (t <= pos1 && (!a.window || t + TOK - 1 > pos0 - a.window)));
+            if (some) {
+                bool plain = whole(t, pages);
+                if (a.causal) plain = plain && t + TOK - 1 <= pos0 && (!a.window || t > pos1 - a.window);
+                take(!plain, t, tile(cur), scales[cur], pages);
+            }
+            if (more) settle(tile(cur ^ 1), scales[cur ^ 1]);
+        }
+    }
+
+    // ---- out ----
+    {
+        unsigned x, y;
+        lane_pair<32>(__builtin_bit_cast(unsigned, l), x, y);
+        l = __builtin_bit_cast(float, x) + __builtin_bit_cast(float, y);
+    }
+    if (it.parts > 1) {
+        if (!live) return;
+        float *out = static_cast<float *>(a.ws) + ((size_t)index * a.kv.heads + kvh) * attn_partial_floats(BM, D);
+        const int r = wave * 32 + col;
+#pragma unroll
+        for (int e = 0; e < ET; ++e)
+#pragma unroll
+            for (int i4 = 0; i4 < 4; ++i4)
+                *reinterpret_cast<f4 *>(out + (size_t)r * D + 32 * e + 8 * i4 + 4 * h) = f4{o[e][4 * i4], o[e][4 * i4 + 1], o[e][4 * i4 + 2], o[e][4 * i4 + 3]};
+        if (h == 0) out[(size_t)BM * D + r] = ELEM == 2 ? m * c : m, out[(size_t)BM * (D + 1) + r] = l;
+        return;
+    }
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    __half *dst = a.y + (int64_t)(it.r.cu + token) * a.ldy + (int64_t)head * D;
+#pragma unroll
+    for (int e = 0; e < ET; ++e)
+#pragma unroll
+        for (int i8 = 0; i8 < 2; ++i8) {
+            // quads 4 h .. of 8 channels each: halves of the wavefront trade, so that every lane stores 8 channels
+            const unsigned a0 = pack2(o[e][8 * i8] * inv, o[e][8 * i8 + 1] * inv), a1 = pack2(o[e][8 * i8 + 2] * inv, o[e][8 * i8 + 3] * inv);
+            const unsigned b0 = pack2(o[e][8 * i8 + 4] * inv, o[e][8 * i8 + 5] * inv), b1 = pack2(o[e][8 * i8 + 6] * inv, o[e][8 * i8 + 7] * inv);
+            const auto x = __builtin_amdgcn_permlane32_swap(a0, b0, false, false), y = __builtin_amdgcn_permlane32_swap(a1, b1, false, false);
+            if (live) *reinterpret_cast<u4 *>(dst + 32 * e + 16 * i8 + 8 * h) = u4{x[0], y[0], x[1], y[1]};
+        }
+}
+
+template <int ELEM, int D>
+int launch(const AttnArgs &a, const AttnPlan &p, float c, unsigned flip, hipStream_t st)
+{
+    constexpr int LDS = 2 * (D == 256 ? 1 : 2) * 32 * D * 4;
+    auto kern = attn_tile_kernel<ELEM, D, 4>;
+    // once per kernel and process; the initialisation of a function-local static is thread-safe
+    static const hipError_t attr_status = hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+    QL_TRY(check_hip(attr_status, "hipFuncSetAttribute(max dynamic LDS)"));
+    kern<<<(unsigned)(p.items * a.kv.heads), 256, LDS, st>>>(a, p, c, flip);
+    return check_hip(hipGetLastError(), "attn_tile_kernel");
+}
+
+}  // namespace
+
+int launch_attention_tiles(const AttnArgs &a, const AttnPlan &p, float c, hipStream_t st)
+{
+    const unsigned flip = a.scale < 0 ? 0x80008000u : 0u;
+    if (a.kv.bits == 16) {
+        if (a.kv.D == 64) return launch<2, 64>(a, p, c, flip, st);
+        if (a.kv.D == 128) return launch<2, 128>(a, p, c, flip, st);
+        return launch<2, 256>(a, p, c, flip, st);
+    }
+    if (a.kv.D == 64) return launch<1, 64>(a, p, c, flip, st);
+    if (a.kv.D == 128) return launch<1, 128>(a, p, c, flip, st);
+    return launch<1, 256>(a, p, c, flip, st);
+}
+
+}  // namespace ql
