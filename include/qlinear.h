@@ -377,7 +377,7 @@ int ql_kv_read(const void *cache, const ql_kv_format *format /* host */, const i
  *   block_table  int32 [requests][ld_table], `columns` of each used;  cu_new int32 [requests + 1]: rows cu_new[b] .. cu_new[b+1] - 1 are
  *                the new tokens of request b, which are not decreasing; rows from cu_new[requests] on are left as they were
  *   ctx_len      int32 [requests]: position of a request's first new token (may be NULL without `causal`)
- *   kv_len       int32 [requests]: tokens in the cache, the new ones among them (at most columns * page_size count)
+ *   kv_len       int32 [requests]: tokens in the cache, the new ones among them (at most columns * page_size count, which is at most 2^30)
  *   max_new      the most new tokens that a request has, as far as the caller knows it (0: not known): goes into the choice of the
  *                kernel, never into the result's correctness
  *   ws           workspace of ql_paged_attention_bytes for the same sizes, 256-byte aligned: partial results of requests whose tokens

@@ -177,6 +177,7 @@ struct AttnPlan {
 };
 AttnPlan attention_plan(const KvView &kv, int T, int requests, int q_heads, int max_new);
 
+int launch_attention_steps(const AttnArgs &a, const AttnPlan &p, float c, hipStream_t st);
 int launch_attention_tiles(const AttnArgs &a, const AttnPlan &p, float c, hipStream_t st);
 
 }  // namespace ql

@@ -70,9 +70,11 @@ AttnPlan attention_plan(const KvView &kv, int T, int requests, int q_heads, int 
 {
     AttnPlan p = {};
     const int group = q_heads / kv.heads;
-    p.bm = 128;
+    const int64_t rows = (int64_t)(max_new && max_new < T ? max_new : T) * group;   // most of a request
+    p.step = rows <= (kv.D == 256 ? 16 : 32);
+    p.bm = !p.step ? 128 : rows <= 16 ? 16 : 32;
     const int64_t tiles = (int64_t)T * group / p.bm + requests;
-    p.target = tiles * kv.heads >= 512 ? 0 : ceil_div(512, kv.heads);
+    p.target = !p.step && tiles * kv.heads >= 512 ? 0 : ceil_div(512, kv.heads);
     p.items = (int)(tiles + p.target);
     p.ws_bytes = p.target ? (size_t)p.items * kv.heads * attn_partial_floats(p.bm, kv.D) * 4 : 0;
     return p;
@@ -90,7 +92,7 @@ int launch_attention(const AttnArgs &a, hipStream_t st)
         return fail(QL_ERR_UNSUPPORTED, "%d tokens of %d query heads are more than a launch holds", a.T, a.q_heads);
     // exp(scale s) = exp2(c s); a scale of nothing keeps masked scores apart from the others (-inf times 0 would be NaN)
     const float c = fmaxf(std::fabs(a.scale) * 1.44269504088896341f, 1e-30f);
-    QL_TRY(launch_attention_tiles(a, p, c, st));
+    QL_TRY(p.step ? launch_attention_steps(a, p, c, st) : launch_attention_tiles(a, p, c, st));
     if (!p.target) return QL_OK;
     if (a.kv.D == 64) attn_join_kernel<64><<<a.T, ATTN_THREADS, 0, st>>>(a, p);
     else if (a.kv.D == 128) attn_join_kernel<128><<<a.T, ATTN_THREADS, 0, st>>>(a, p);

@@ -216,8 +216,8 @@ int ql_paged_attention(const void *q, int64_t ldq, int T, int q_heads, const voi
     if (window < 0 || (window && !causal)) return fail(QL_ERR_SHAPE, "window=%d must not be negative, and 0 without causal", window);
     if (T == 0 || requests == 0) return QL_OK;
     QL_TRY(check_cache(cache));
-    if (columns < 1 || (int64_t)columns * format->page_size >= ((int64_t)1 << 31))
-        return fail(QL_ERR_SHAPE, "columns=%d must be positive and columns * page_size below 2^31", columns);
+    if (columns < 1 || (int64_t)columns * format->page_size > ((int64_t)1 << 30))
+        return fail(QL_ERR_SHAPE, "columns=%d must be positive and columns * page_size at most 2^30", columns);
     if (ld_table < columns) return fail(QL_ERR_SHAPE, "ld_table=%lld is less than columns=%d", (long long)ld_table, columns);
     QL_TRY(check_ints(block_table, "block_table"));
     QL_TRY(check_ints(cu_new, "cu_new"));
