@@ -165,8 +165,11 @@ __device__ inline void attn_part_range(int &low, int &high, int part, int parts)
     high = min(high, l0 + (int)((int64_t)u * (part + 1) / parts) * ATTN_UNIT);
 }
 
-// Partial results of an item: bm rows of D fp32 sums, then bm maxima (in powers of two) and bm sums of the weights.
+// Workspace: for every item a note of what there is to join (int4: parts, or 0 where this item is not the first of several; first row
+// of q, first row of the tile, rows of the request), then for every item and key/value head bm rows of D fp32 sums, bm maxima (in powers
+// of two) and bm sums of the weights.
 __host__ __device__ inline size_t attn_partial_floats(int bm, int D) { return (size_t)bm * (D + 2); }
+__host__ __device__ inline size_t attn_notes_bytes(int items) { return ((size_t)items * 16 + 255) & ~(size_t)255; }
 
 struct AttnPlan {
     int bm;              // rows of a tile
@@ -176,6 +179,21 @@ struct AttnPlan {
     size_t ws_bytes;
 };
 AttnPlan attention_plan(const KvView &kv, int T, int requests, int q_heads, int max_new);
+
+__device__ inline float *attn_partial(const AttnArgs &a, const AttnPlan &p, int64_t item, int kvh)
+{
+    return reinterpret_cast<float *>(static_cast<char *>(a.ws) + attn_notes_bytes(p.items)) + (item * a.kv.heads + kvh) * attn_partial_floats(p.bm, a.kv.D);
+}
+
+// Finds the workgroup's item and leaves the note of it.
+template <int THREADS>
+__device__ inline bool attn_take(const AttnArgs &a, const AttnPlan &p, int64_t index, int kvh, AttnScratch &s, AttnItem &it)
+{
+    const bool there = attn_item<THREADS>(a, p.bm, p.target, index, s, it);
+    if (p.target && kvh == 0 && threadIdx.x == 0)
+        static_cast<int4 *>(a.ws)[index] = there && it.part == 0 && it.parts > 1 ? make_int4(it.parts, it.r.cu, it.tile * p.bm, it.r.rows) : make_int4(0, 0, 0, 0);
+    return there;
+}
 
 int launch_attention_steps(const AttnArgs &a, const AttnPlan &p, float c, hipStream_t st);
 int launch_attention_tiles(const AttnArgs &a, const AttnPlan &p, float c, hipStream_t st);

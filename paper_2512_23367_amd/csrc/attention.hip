@@ -6,61 +6,52 @@
 namespace ql {
 namespace {
 
-// Joins the parts of the rows whose tokens several workgroups shared: one workgroup per new token, a wavefront per query head in turn.
+// Joins the parts of the rows whose tokens several workgroups shared: a wavefront takes `rows` / 4 rows of an item and key/value head in
+// turn, its lanes the channels; the weights of the parts (lane k: part k) first, so that the loads of the sums wait for nothing.
 template <int D>
-__global__ __launch_bounds__(ATTN_THREADS) void attn_join_kernel(AttnArgs a, AttnPlan plan)
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, AttnPlan plan, int rows)
 {
     constexpr int N = D / 64;
-    __shared__ AttnScratch scratch;
-    __shared__ int owner;
-    const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    int64_t tiles;
-    const int64_t work = attn_work<ATTN_THREADS>(a, plan.bm, scratch.part, tiles);
-    const int c = attn_part_units(work, plan.target);
-    // t's request, and the items before it
-    if (tid == 0) owner = -1;
-    __syncthreads();
-    for (int b = tid; b < a.requests; b += ATTN_THREADS) {
-        const AttnSpan r = attn_span(a, b);
-        if (t >= r.cu && t < r.cu + r.rows / a.group) owner = b;
-    }
-    __syncthreads();
-    const int b = owner;
-    if (b < 0) return;
-    const AttnSpan r = attn_span(a, b);
-    const int parts = attn_parts(r, c);
-    if (parts == 1) return;
-    int64_t n = 0, before;
-    for (int i = tid; i < b; i += ATTN_THREADS) {
-        const AttnSpan s = attn_span(a, i);
-        n += (int64_t)attn_tiles(s, plan.bm) * attn_parts(s, c);
-    }
-    block_sum_before<ATTN_THREADS>(n, scratch.part, before);
-
-    const size_t size = attn_partial_floats(plan.bm, D);
-    for (int head = wave; head < a.q_heads; head += ATTN_THREADS / 64) {
-        const int kvh = head / a.group, row = (t - r.cu) * a.group + head % a.group;
-        const int64_t item = before + (int64_t)(row / plan.bm) * parts;
-        if (item + parts > plan.items) continue;             // (lengths that contradict each other)
-        const float *p0 = static_cast<const float *>(a.ws) + ((size_t)item * a.kv.heads + kvh) * size;
-        const size_t step = (size_t)a.kv.heads * size;
-        const int at = row % plan.bm;
+    typedef float fn __attribute__((ext_vector_type(N)));
+    const int kvh = blockIdx.x % a.kv.heads, item = blockIdx.x / a.kv.heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int4 note = static_cast<const int4 *>(a.ws)[item];
+    const int parts = min(note.x, plan.items - item);
+    if (parts < 2) return;
+    const size_t step = (size_t)a.kv.heads * attn_partial_floats(plan.bm, D);
+    for (int at = blockIdx.y * rows + wave; at < min((int)(blockIdx.y + 1) * rows, plan.bm); at += 4) {
+        const int row = note.z + at;
+        if (row >= note.w) return;
+        const float *p0 = attn_partial(a, plan, item, kvh), *pm = p0 + (size_t)plan.bm * D + at, *ps = p0 + (size_t)at * D + lane * N;
         float m = -INFINITY;
-        for (int k = 0; k < parts; ++k) m = fmaxf(m, p0[k * step + (size_t)plan.bm * D + at]);
+        for (int k = lane; k < parts; k += 64) m = fmaxf(m, pm[k * step]);
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
         float l = 0, o[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) o[i] = 0;
-        for (int k = 0; k < parts; ++k) {
-            const float *p = p0 + k * step;
-            const float mk = p[(size_t)plan.bm * D + at], lk = p[(size_t)plan.bm * (D + 1) + at];
-            const float w = lk == 0.f ? 0.f : __builtin_amdgcn_exp2f(mk - m);
+        for (int k0 = 0; k0 < parts; k0 += 64) {
+            const int k = k0 + lane;
+            const float lk = k < parts ? pm[k * step + plan.bm] : 0.f;
+            const float w = lk == 0.f ? 0.f : __builtin_amdgcn_exp2f(pm[k * step] - m);   // (lk 0: nothing seen, its sums are 0; NaN stays)
             l += lk * w;
+            for (int i0 = 0; i0 < min(parts - k0, 64); i0 += 8) {             // (behind the last part: the last one again, with weight 0)
+                fn v[8];
 #pragma unroll
-            for (int i = 0; i < N; ++i) o[i] = fmaf(lk == 0.f ? 0.f : p[(size_t)at * D + lane + 64 * i], w, o[i]);
+                for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const fn *>(ps + min(k0 + i0 + i, parts - 1) * step);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float wi = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), i0 + i));
+#pragma unroll
+                    for (int c = 0; c < N; ++c) o[c] = fmaf(v[i][c], wi, o[c]);
+                }
+            }
         }
-        const float inv = l == 0.f ? 0.f : 1.0f / l;
 #pragma unroll
-        for (int i = 0; i < N; ++i) a.y[(int64_t)t * a.ldy + (int64_t)head * D + lane + 64 * i] = __float2half(o[i] * inv);
+        for (int d = 1; d < 64; d *= 2) l += __shfl_xor(l, d);
+        const float inv = l == 0.f ? 0.f : 1.0f / l;
+        __half *dst = a.y + (int64_t)(note.y + row / a.group) * a.ldy + (int64_t)(kvh * a.group + row % a.group) * D + lane * N;
+#pragma unroll
+        for (int c = 0; c < N; ++c) dst[c] = __float2half(o[c] * inv);
     }
 }
 
@@ -76,7 +67,7 @@ AttnPlan attention_plan(const KvView &kv, int T, int requests, int q_heads, int 
     const int64_t tiles = (int64_t)T * group / p.bm + requests;
     p.target = !p.step && tiles * kv.heads >= 512 ? 0 : ceil_div(512, kv.heads);
     p.items = (int)(tiles + p.target);
-    p.ws_bytes = p.target ? (size_t)p.items * kv.heads * attn_partial_floats(p.bm, kv.D) * 4 : 0;
+    p.ws_bytes = p.target ? attn_notes_bytes(p.items) + (size_t)p.items * kv.heads * attn_partial_floats(p.bm, kv.D) * 4 : 0;
     return p;
 }
 
@@ -94,9 +85,11 @@ int launch_attention(const AttnArgs &a, hipStream_t st)
     const float c = fmaxf(std::fabs(a.scale) * 1.44269504088896341f, 1e-30f);
     QL_TRY(p.step ? launch_attention_steps(a, p, c, st) : launch_attention_tiles(a, p, c, st));
     if (!p.target) return QL_OK;
-    if (a.kv.D == 64) attn_join_kernel<64><<<a.T, ATTN_THREADS, 0, st>>>(a, p);
-    else if (a.kv.D == 128) attn_join_kernel<128><<<a.T, ATTN_THREADS, 0, st>>>(a, p);
-    else attn_join_kernel<256><<<a.T, ATTN_THREADS, 0, st>>>(a, p);
+    const int rows = p.step ? 4 : 16;
+    const dim3 grid(p.items * a.kv.heads, p.bm / rows);
+    if (a.kv.D == 64) attn_join_kernel<64><<<grid, 256, 0, st>>>(a, p, rows);
+    else if (a.kv.D == 128) attn_join_kernel<128><<<grid, 256, 0, st>>>(a, p, rows);
+    else attn_join_kernel<256><<<grid, 256, 0, st>>>(a, p, rows);
     return check_hip(hipGetLastError(), "attn_join_kernel");
 }
 

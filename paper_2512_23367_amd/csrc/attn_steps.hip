@@ -43,7 +43,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attn_step_kernel(AttnAr
 
     const int kvh = blockIdx.x % a.kv.heads, index = blockIdx.x / a.kv.heads;
     AttnItem it;
-    if (!attn_item<NW * 64>(a, BM, plan.target, index, scratch, it)) return;
+    if (!attn_take<NW * 64>(a, plan, index, kvh, scratch, it)) return;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, qd = lane >> 4;
     const int row0 = it.tile * BM;
@@ -290,7 +290,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attn_step_kernel(AttnAr
         for (int e = 0; e < ET; ++e) o[n][e] *= w;
     }
     const bool partial = it.parts > 1;
-    float *out = partial ? static_cast<float *>(a.ws) + ((size_t)index * a.kv.heads + kvh) * attn_partial_floats(BM, D) : nullptr;
+    float *out = partial ? attn_partial(a, plan, index, kvh) : nullptr;
 #pragma unroll
     for (int e0 = 0; e0 < ET; e0 += EP) {
 #pragma unroll

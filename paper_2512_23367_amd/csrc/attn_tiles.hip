@@ -32,7 +32,7 @@ __global__ __launch_bounds__(NW * 64, D == 256 ? 1 : 2) void attn_tile_kernel(At
 
     const int kvh = blockIdx.x % a.kv.heads, index = blockIdx.x / a.kv.heads;
     AttnItem it;
-    if (!attn_item<NW * 64>(a, BM, plan.target, index, scratch, it)) return;
+    if (!attn_take<NW * 64>(a, plan, index, kvh, scratch, it)) return;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, h = lane >> 5;
     const int row0 = it.tile * BM, wrow0 = row0 + wave * 32, row = wrow0 + col;
@@ -273,7 +273,7 @@ __global__ __launch_bounds__(NW * 64, D == 256 ? 1 : 2) void attn_tile_kernel(At
     }
     if (it.parts > 1) {
         if (!live) return;
-        float *out = static_cast<float *>(a.ws) + ((size_t)index * a.kv.heads + kvh) * attn_partial_floats(BM, D);
+        float *out = attn_partial(a, plan, index, kvh);
         const int r = wave * 32 + col;
 #pragma unroll
         for (int e = 0; e < ET; ++e)
