@@ -136,7 +136,9 @@ def _bind_native(l):
                       f"torch? rebuild with `python -m paper_2512_23367_amd.build`): {e}", RuntimeWarning)
         return
     names = ("ql_weight_bytes", "ql_act_kernel_bytes", "ql_w8a8_linear", "ql_w4a8_linear", "ql_w8a8_gemm", "ql_w4a8_gemm",
-             "ql_quant_act_per_token", "ql_quant_act_rmsnorm", "ql_quant_act_swiglu", "ql_quant_act_per_token_transformed")
+             "ql_quant_act_per_token", "ql_quant_act_rmsnorm", "ql_quant_act_swiglu", "ql_quant_act_per_token_transformed",
+             "ql_kv_cache_bytes", "ql_kv_resize", "ql_kv_append", "ql_kv_read", "ql_paged_attention")
+    _qlcall.bind_format(QlKvFormat)
     _qlcall.bind(tuple(ctypes.cast(getattr(l, n), ctypes.c_void_p).value for n in names))
     _native = _qlcall
 
@@ -463,8 +465,8 @@ def _heads_of(t, name, rows, head_dim):
 
 
 def _row_stride(t):
-    """The leading dimension of a checked matrix (torch gives a single row any stride: its columns do as well)."""
-    return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else (t.shape[1] + 7) // 8 * 8
+    """The leading dimension of a checked matrix (torch gives a single row any stride: its columns, rounded up, do as well)."""
+    return t.stride(0) if t.shape[0] > 1 else (t.shape[1] + 7) // 8 * 8
 
 
 def _kv_rows(t, name, rows, fmt):
@@ -493,12 +495,14 @@ def _table(t, requests):
     _want(t, torch.int32, "block_table")
     if t.dim() != 2 or t.shape[0] < requests or (t.numel() and t.stride(1) != 1):
         raise ValueError(f"block_table must be [{requests}, columns] with unit inner stride")
-    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])), t.shape[1]
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else t.shape[1]), t.shape[1]
 
 
 def ql_kv_resize(page_size, old_len, want_len, ring, pool, pool_out, block_table, kv_len, cu_new, slots, positions):
     """Pages, slots and positions for requests that go from old_len to want_len tokens; all int32 tensors on the device.
     The pool has ring.numel() pages; slots and positions have room for the step's new tokens."""
+    if _native is not None and _done(_native.kv_resize(page_size, old_len, want_len, ring, pool, pool_out, block_table, kv_len, cu_new, slots, positions, _stream)):
+        return
     _here(old_len, want_len, ring, pool, pool_out, block_table, kv_len, cu_new, slots, positions)
     n, most = old_len.numel(), min(slots.numel(), positions.numel())
     table, ld, columns = _table(block_table, n)
@@ -509,6 +513,8 @@ def ql_kv_resize(page_size, old_len, want_len, ring, pool, pool_out, block_table
 
 def ql_kv_append(q, k, v, cos_sin, positions, slots, q_out, cache, fmt):
     """Rotates q (into q_out, which may be q) and k by cos_sin (fp32 [positions, rotary_dim], or None) and stores k and v."""
+    if _native is not None and _done(_native.kv_append(q, k, v, cos_sin, positions, slots, q_out, cache, fmt, _stream)):
+        return
     _here(q, k, v, cos_sin, positions, slots, q_out, cache)
     T = k.shape[0]
     _kv_rows(k, "k", T, fmt), _kv_rows(v, "v", T, fmt)
@@ -530,6 +536,8 @@ def ql_kv_append(q, k, v, cos_sin, positions, slots, q_out, cache, fmt):
 
 def ql_kv_read(cache, fmt, slots, k=None, v=None):
     """Keys and values of the given slots as fp16 [T, heads * head_dim] (either may be None)."""
+    if _native is not None and _done(_native.kv_read(cache, fmt, slots, k, v, _stream)):
+        return
     _here(cache, slots, k, v)
     T = (k if k is not None else v if v is not None else slots).shape[0]
     for t, name in ((k, "k"), (v, "v")):
@@ -547,6 +555,8 @@ def ql_paged_attention_bytes(fmt: QlKvFormat, T: int, requests: int, q_heads: in
 
 def ql_paged_attention(q, cache, fmt, block_table, cu_new, ctx_len, kv_len, scale, y, ws=None, causal=True, window=0, max_new=0):
     """Attention of the new tokens q (rows cu_new[b] .. of request b) over the cache; ws: ql_paged_attention_bytes of the same sizes."""
+    if _native is not None and _done(_native.paged_attention(q, cache, fmt, block_table, cu_new, ctx_len, kv_len, scale, y, ws, causal, window, max_new, _stream)):
+        return
     _here(q, cache, block_table, cu_new, ctx_len, kv_len, y, ws)
     T, n = q.shape[0], kv_len.numel()
     q_heads = _heads_of(q, "q", T, fmt.head_dim)

@@ -6,11 +6,13 @@
 //
 // Lengths are known on the device only (a captured step is replayed with others).  The host launches as many workgroups as the sizes
 // that it knows allow for, and each finds its work from the lengths: request b has tiles_b = ceil(new_b G / bm) tiles and
-// parts_b = ceil(units_b / C) parts of each (units of 64 tokens), C chosen so that all tiles and heads together have about `target`
-// parts: sum tiles_b parts_b <= target + sum tiles_b <= target + floor(T G / bm) + requests.  Without parts (target 0): one per tile.
+// parts_b = ceil(units_b / C) parts of each (units of 64 tokens); see attn_part_units for C.  Without parts (slots 0): one per tile.
 #pragma once
 
+#include <type_traits>
+
 #include "kv_cache.h"
+#include "quant_math.h"
 
 namespace ql {
 
@@ -51,6 +53,58 @@ __device__ inline AttnSpan attn_span(const AttnArgs &a, int b)
 
 __device__ inline int attn_units(int low, int high) { return (max(high - low, 0) + ATTN_UNIT - 1) / ATTN_UNIT; }
 
+__device__ inline int attn_tiles(const AttnSpan &r, int bm) { return (r.rows + bm - 1) / bm; }
+
+struct AttnTotals {
+    int64_t tiles, work;                 // tiles; tiles x units
+    int most;                            // units of a tile
+};
+
+// Units of a part, from the totals and the number of workgroups of a key/value head that run at the same time (`slots`).  In k rounds
+// over the slots there is room for k slots - tiles cuts, so that parts of work / (k slots - tiles) units suffice; each part costs
+// about two units on top (finding its work, the queries, joining).  One round, or two if that is shorter; where the tiles alone fill
+// the slots, parts of what a slot has on average.  No more than max(2 slots, tiles + slots) parts in all.
+// Decode steps, 8 heads, int8, against parts of work / slots units (a few more of them than slots): four requests of 60000..131072
+// tokens 150 us, 181; 32 requests of 200..4096 tokens 33 us, 39.
+constexpr int ATTN_LEAST = 4;
+__device__ inline int attn_part_units(const AttnTotals &t, int slots)
+{
+    if (slots == 0) return 1 << 30;
+    int64_t c;
+    if (t.tiles >= slots) {
+        c = (t.work + slots - 1) / slots;
+    } else {
+        const int64_t r1 = slots - t.tiles, r2 = 2 * (int64_t)slots - t.tiles;
+        const int64_t c1 = (t.work + r1 - 1) / r1, c2 = (t.work + r2 - 1) / r2;
+        c = min(c1, (int64_t)t.most) + 2 <= 2 * (min(c2, (int64_t)t.most) + 2) ? c1 : c2;
+    }
+    return (int)min(max(c, (int64_t)ATTN_LEAST), (int64_t)1 << 30);
+}
+__device__ inline int attn_parts(const AttnSpan &r, int part_units) { return max(1, (attn_units(r.low, r.high) + part_units - 1) / part_units); }
+
+__device__ inline int64_t wave_total(int64_t v)
+{
+    auto step = [&](auto off) {
+        unsigned a, b, c, d;
+        lane_pair<decltype(off)::value>((unsigned)v, a, b);
+        lane_pair<decltype(off)::value>((unsigned)((uint64_t)v >> 32), c, d);
+        v = (int64_t)((uint64_t)c << 32 | a) + (int64_t)((uint64_t)d << 32 | b);
+    };
+    step(std::integral_constant<int, 1>{}), step(std::integral_constant<int, 2>{}), step(std::integral_constant<int, 4>{});
+    step(std::integral_constant<int, 8>{}), step(std::integral_constant<int, 16>{}), step(std::integral_constant<int, 32>{});
+    return v;
+}
+__device__ inline int wave_most(int v)
+{
+    auto step = [&](auto off) {
+        unsigned a, b;
+        lane_pair<decltype(off)::value>((unsigned)v, a, b);
+        v = max((int)a, (int)b);
+    };
+    step(std::integral_constant<int, 1>{}), step(std::integral_constant<int, 2>{}), step(std::integral_constant<int, 4>{});
+    step(std::integral_constant<int, 8>{}), step(std::integral_constant<int, 16>{}), step(std::integral_constant<int, 32>{});
+    return v;
+}
 __device__ inline int64_t wave_sum_before(int64_t v, int lane)    // inclusive prefix sum over a wavefront
 {
 #pragma unroll
@@ -60,89 +114,94 @@ __device__ inline int64_t wave_sum_before(int64_t v, int lane)    // inclusive p
     }
     return v;
 }
+__device__ inline int wave_sum_before(int v, int lane)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int o = __shfl_up(v, d);
+        if (lane >= d) v += o;
+    }
+    return v;
+}
 
 struct AttnScratch {
-    int64_t part[ATTN_THREADS / 64];
-    int64_t found[3];
+    int64_t part[3][ATTN_THREADS / 64];
+    int64_t found[2];
 };
-
-// exclusive prefix sum over the workgroup's THREADS threads, and its total
-template <int THREADS>
-__device__ inline int64_t block_sum_before(int64_t v, int64_t *part, int64_t &sum)
-{
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t inc = wave_sum_before(v, lane);
-    __syncthreads();
-    if (lane == 63) part[wave] = inc;
-    __syncthreads();
-    int64_t before = 0;
-    sum = 0;
-#pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) {
-        if (w < wave) before += part[w];
-        sum += part[w];
-    }
-    return before + inc - v;
-}
-
-__device__ inline int attn_tiles(const AttnSpan &r, int bm) { return (r.rows + bm - 1) / bm; }
-
-// units of a part, from the sum over all requests of tiles x units
-__device__ inline int attn_part_units(int64_t work, int target)
-{
-    const int64_t c = target ? (work + target - 1) / target : (int64_t)1 << 30;
-    return (int)min(max(c, (int64_t)4), (int64_t)1 << 30);
-}
-__device__ inline int attn_parts(const AttnSpan &r, int part_units) { return max(1, (attn_units(r.low, r.high) + part_units - 1) / part_units); }
-
-template <int THREADS>
-__device__ inline int64_t attn_work(const AttnArgs &a, int bm, int64_t *part, int64_t &tiles)
-{
-    int64_t work = 0, n = 0, sum;
-    for (int b = threadIdx.x; b < a.requests; b += THREADS) {
-        const AttnSpan r = attn_span(a, b);
-        n += attn_tiles(r, bm);
-        work += (int64_t)attn_tiles(r, bm) * attn_units(r.low, r.high);
-    }
-    block_sum_before<THREADS>(n, part, tiles);
-    block_sum_before<THREADS>(work, part, sum);
-    return sum;
-}
 
 // The item-th tile (and part) of all requests; false if there are fewer.  Without parts the last tile of the last request comes first:
 // causal tiles get longer towards the end of a request, and the longest should not start last.
+// Up to 64 requests every wavefront finds it by itself, a request per lane; more are shared out over the workgroup.
 template <int THREADS>
-__device__ inline bool attn_item(const AttnArgs &a, int bm, int target, int64_t item, AttnScratch &s, AttnItem &out)
+__device__ inline bool attn_item(const AttnArgs &a, int bm, int slots, int item, AttnScratch &s, AttnItem &out)
 {
-    int64_t tiles;
-    const int64_t work = attn_work<THREADS>(a, bm, s.part, tiles);
-    const int c = attn_part_units(work, target);
-    if (target == 0) {
-        if (item >= tiles) return false;
-        item = tiles - 1 - item;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr int NW = THREADS / 64;
+    AttnTotals all;
+    if (a.requests <= 64) {
+        AttnSpan r = {};
+        if (lane < a.requests) r = attn_span(a, lane);
+        const int tiles = attn_tiles(r, bm), units = attn_units(r.low, r.high);
+        all = {wave_total(tiles), slots ? wave_total((int64_t)tiles * units) : 0, slots ? wave_most(units) : 0};
+        const int c = attn_part_units(all, slots), parts = slots ? attn_parts(r, c) : 1;
+        // (at most 2^24 each: more is a cu_new that decreases somewhere)
+        const int n = lane < a.requests ? (int)min((int64_t)tiles * parts, (int64_t)1 << 24) : 0;
+        if (slots == 0) item = (int)min(all.tiles, (int64_t)1 << 30) - 1 - item;
+        const int upto = wave_sum_before(n, lane);
+        const uint64_t owner = __ballot(item >= 0 && item < upto);
+        if (!owner) return false;
+        out.b = __builtin_ctzll(owner);
+        auto of = [&](int v) { return __builtin_amdgcn_readlane(v, out.b); };
+        out.r = {of(r.cu), of(r.rows), of(r.ctx), of(r.len), of(r.low), of(r.high)};
+        out.parts = of(parts);
+        const int k = item - (of(upto) - of(n));
+        out.tile = k / out.parts, out.part = k % out.parts;
+        return true;
     }
+    int64_t tiles = 0, work = 0;
+    int most = 0;
+    for (int b = threadIdx.x; b < a.requests; b += THREADS) {
+        const AttnSpan r = attn_span(a, b);
+        const int n = attn_tiles(r, bm), units = attn_units(r.low, r.high);
+        tiles += n, work += (int64_t)n * units, most = max(most, units);
+    }
+    tiles = wave_total(tiles), work = wave_total(work), most = wave_most(most);
+    if (lane == 0) s.part[0][wave] = tiles, s.part[1][wave] = work, s.part[2][wave] = most;
     if (threadIdx.x == 0) s.found[0] = -1;
-    int64_t before = 0;
-    for (int base = 0; base < a.requests && before <= item; base += THREADS) {
+    __syncthreads();
+    all = {};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) all.tiles += s.part[0][w], all.work += s.part[1][w], all.most = max(all.most, (int)s.part[2][w]);
+    const int c = attn_part_units(all, slots);
+    int64_t want = item, before = 0;
+    if (slots == 0) want = all.tiles - 1 - item;
+    for (int base = 0; base < a.requests && before <= want; base += THREADS) {
         const int b = base + threadIdx.x;
-        int64_t n = 0, sum;
+        int64_t n = 0;
         if (b < a.requests) {
             const AttnSpan r = attn_span(a, b);
-            n = (int64_t)attn_tiles(r, bm) * (target ? attn_parts(r, c) : 1);
+            n = (int64_t)attn_tiles(r, bm) * (slots ? attn_parts(r, c) : 1);
         }
-        const int64_t at = before + block_sum_before<THREADS>(n, s.part, sum);
-        if (item >= at && item < at + n) s.found[0] = b, s.found[1] = item - at;
-        before += sum;
+        const int64_t upto = wave_sum_before(n, lane);
+        __syncthreads();                                     // the sums of the round before have been read
+        if (lane == 63) s.part[0][wave] = upto;
+        __syncthreads();
+        int64_t at = before + upto - n;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            if (w < wave) at += s.part[0][w];
+            before += s.part[0][w];
+        }
+        if (want >= at && want < at + n) s.found[0] = b, s.found[1] = want - at;
     }
     __syncthreads();
     out.b = __builtin_amdgcn_readfirstlane((int)s.found[0]);
     if (out.b < 0) return false;
     const int k = __builtin_amdgcn_readfirstlane((int)s.found[1]);
-    out.r = attn_span(a, out.b);
-    out.r.cu = __builtin_amdgcn_readfirstlane(out.r.cu), out.r.rows = __builtin_amdgcn_readfirstlane(out.r.rows);
-    out.r.ctx = __builtin_amdgcn_readfirstlane(out.r.ctx), out.r.len = __builtin_amdgcn_readfirstlane(out.r.len);
-    out.r.low = __builtin_amdgcn_readfirstlane(out.r.low), out.r.high = __builtin_amdgcn_readfirstlane(out.r.high);
-    out.parts = __builtin_amdgcn_readfirstlane(target ? attn_parts(out.r, c) : 1);
+    const AttnSpan r = attn_span(a, out.b);
+    auto same = [&](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    out.r = {same(r.cu), same(r.rows), same(r.ctx), same(r.len), same(r.low), same(r.high)};
+    out.parts = same(slots ? attn_parts(out.r, c) : 1);
     out.tile = k / out.parts, out.part = k % out.parts;
     return true;
 }
@@ -174,7 +233,7 @@ __host__ __device__ inline size_t attn_notes_bytes(int items) { return ((size_t)
 struct AttnPlan {
     int bm;              // rows of a tile
     int step;            // 1: the kernel for few rows, whose wavefronts share a tile's tokens
-    int target;          // parts that all tiles of a key/value head together are cut into (0: none)
+    int slots;           // workgroups of a key/value head that run at the same time (0: a workgroup per tile, no parts)
     int items;           // workgroups of a key/value head
     size_t ws_bytes;
 };
@@ -187,10 +246,10 @@ __device__ inline float *attn_partial(const AttnArgs &a, const AttnPlan &p, int6
 
 // Finds the workgroup's item and leaves the note of it.
 template <int THREADS>
-__device__ inline bool attn_take(const AttnArgs &a, const AttnPlan &p, int64_t index, int kvh, AttnScratch &s, AttnItem &it)
+__device__ inline bool attn_take(const AttnArgs &a, const AttnPlan &p, int index, int kvh, AttnScratch &s, AttnItem &it)
 {
-    const bool there = attn_item<THREADS>(a, p.bm, p.target, index, s, it);
-    if (p.target && kvh == 0 && threadIdx.x == 0)
+    const bool there = attn_item<THREADS>(a, p.bm, p.slots, index, s, it);
+    if (p.slots && kvh == 0 && threadIdx.x == 0)
         static_cast<int4 *>(a.ws)[index] = there && it.part == 0 && it.parts > 1 ? make_int4(it.parts, it.r.cu, it.tile * p.bm, it.r.rows) : make_int4(0, 0, 0, 0);
     return there;
 }

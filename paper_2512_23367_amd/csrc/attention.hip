@@ -65,9 +65,11 @@ AttnPlan attention_plan(const KvView &kv, int T, int requests, int q_heads, int 
     p.step = rows <= (kv.D == 256 ? 16 : 32);
     p.bm = !p.step ? 128 : rows <= 16 ? 16 : 32;
     const int64_t tiles = (int64_t)T * group / p.bm + requests;
-    p.target = !p.step && tiles * kv.heads >= 512 ? 0 : ceil_div(512, kv.heads);
-    p.items = (int)(tiles + p.target);
-    p.ws_bytes = p.target ? attn_notes_bytes(p.items) + (size_t)p.items * kv.heads * attn_partial_floats(p.bm, kv.D) * 4 : 0;
+    // workgroups that the registers of a kernel leave room for on a CU, times 256 CUs
+    const int resident = 256 * (kv.D == 256 ? 1 : p.bm == 16 && kv.bits == 16 ? 3 : 2);
+    p.slots = !p.step && tiles * kv.heads >= resident ? 0 : ceil_div(resident, kv.heads);
+    p.items = (int)(p.slots ? (2 * (int64_t)p.slots > tiles + p.slots ? 2 * (int64_t)p.slots : tiles + p.slots) : tiles);
+    p.ws_bytes = p.slots ? attn_notes_bytes(p.items) + (size_t)p.items * kv.heads * attn_partial_floats(p.bm, kv.D) * 4 : 0;
     return p;
 }
 
@@ -84,7 +86,7 @@ int launch_attention(const AttnArgs &a, hipStream_t st)
     // exp(scale s) = exp2(c s); a scale of nothing keeps masked scores apart from the others (-inf times 0 would be NaN)
     const float c = fmaxf(std::fabs(a.scale) * 1.44269504088896341f, 1e-30f);
     QL_TRY(p.step ? launch_attention_steps(a, p, c, st) : launch_attention_tiles(a, p, c, st));
-    if (!p.target) return QL_OK;
+    if (!p.slots) return QL_OK;
     const int rows = p.step ? 4 : 16;
     const dim3 grid(p.items * a.kv.heads, p.bm / rows);
     if (a.kv.D == 64) attn_join_kernel<64><<<grid, 256, 0, st>>>(a, p, rows);

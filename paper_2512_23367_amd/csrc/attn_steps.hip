@@ -1,7 +1,6 @@
 // Attention of few new tokens over the paged cache (decode steps, drafts): the four wavefronts of a workgroup share out the tokens and
 // stream keys and values from memory straight to registers.
 #include "attention.h"
-#include "quant_math.h"
 
 namespace ql {
 namespace {

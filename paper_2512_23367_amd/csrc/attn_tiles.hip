@@ -2,7 +2,6 @@
 // in LDS.
 #include "attention.h"
 #include "gemm_tiles.h"
-#include "quant_math.h"
 
 namespace ql {
 namespace {

@@ -188,8 +188,8 @@ static int check_attention_sizes(const KvView &kv, int T, int requests, int q_he
     if (T < 0 || requests < 0 || max_new < 0)
         return fail(QL_ERR_SHAPE, "T=%d, requests=%d and max_new=%d must not be negative", T, requests, max_new);
     QL_TRY(check_q_heads(q_heads, kv.heads));
-    if (requests > 65536 || (int64_t)T * (q_heads / kv.heads) >= ((int64_t)1 << 30))
-        return fail(QL_ERR_UNSUPPORTED, "at most 65536 requests (requests=%d) and T * q_heads / heads below 2^30", requests);
+    if (requests > 65536 || (int64_t)T * (q_heads / kv.heads) >= ((int64_t)1 << 28))
+        return fail(QL_ERR_UNSUPPORTED, "at most 65536 requests (requests=%d) and T * q_heads / heads below 2^28", requests);
     return QL_OK;
 }
 

@@ -1,5 +1,8 @@
 // Bookkeeping of the paged key/value cache, and what writes and reads it (layout: include/qlinear.h, kv_cache.h).
+#include <type_traits>
+
 #include "kv_cache.h"
+#include "quant_math.h"
 
 namespace ql {
 namespace {
@@ -148,126 +151,309 @@ __global__ __launch_bounds__(RESIZE_THREADS) void kv_resize_kernel(const int32_t
     }
 }
 
-// ---- new tokens into the cache ---------------------------------------------------------------------------------
+// ---- rows into the cache, and back -----------------------------------------------------------------------------
+// Bound by memory: rows of 2 D bytes are read, blocks written (read back: the other way round).  A workgroup takes 32 consecutive rows of one
+// key/value head, 16 channels per thread: the rows and the keys' pieces are 16 bytes per lane on both sides.  Values lie transposed in
+// a block: they go through LDS, and leave (arrive) 16 bytes at a time where the rows fill the piece of a channel -- 8 tokens in fp16, 16 in
+// int8 --, else by groups of 4 tokens, else singly: a decode step's tokens are single ones, a prompt's rows have them at its ends only.
+// 4096 tokens, 32 + 2 x 32 heads of 128, fp16, and 16001 tokens, 32 + 2 x 8 heads, int8; append / read back, us:  APPEND_FIGURES
+constexpr int TILE = 32;
 
 __device__ inline bool finite(float x) { return __builtin_fabsf(x) <= 3.402823466e38f; }
 
-__device__ inline float wave_max(float v)
+// the D / 16 lanes that hold a token
+template <int LANES, typename OP>
+__device__ inline float over_lanes(float v, OP op)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) v = fmaxf(v, __shfl_xor(v, d));
+    auto step = [&](auto off) {
+        unsigned a, b;
+        lane_pair<decltype(off)::value>(__builtin_bit_cast(unsigned, v), a, b);
+        v = op(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+    };
+    step(std::integral_constant<int, 1>{}), step(std::integral_constant<int, 2>{});
+    if constexpr (LANES >= 8) step(std::integral_constant<int, 4>{});
+    if constexpr (LANES >= 16) step(std::integral_constant<int, 8>{});
     return v;
 }
 
-// One wavefront per token and head; lane l holds channels l, l + 64, ...
-template <int ELEM, int D>
-__global__ __launch_bounds__(256) void kv_append_kernel(const __half *q, int64_t ldq, const __half *__restrict__ k, int64_t ldk,
-                                                        const __half *__restrict__ v, int64_t ldv, int T, int q_heads,
-                                                        const float *__restrict__ cos_sin, int rotary, int max_positions,
-                                                        const int32_t *__restrict__ positions, const int32_t *__restrict__ slots, __half *q_out,
-                                                        int64_t ldqo, KvView kv)
+// How the 32 rows' values lie in their blocks: pieces to move, {row of the first token, kind}.
+enum { ONE = 1, FOUR = 2, WHOLE = 3 };
+struct Pieces {
+    int slot[TILE];                                       // -1: none
+    int count, row[TILE], kind[TILE];
+};
+
+// by the first wavefront
+template <int ELEM>
+__device__ inline void find_pieces(Pieces &p, const int32_t *slots, int t0, int T, const KvView &kv)
 {
-    constexpr int N = D / 64;
-    const int lane = threadIdx.x & 63, t = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (t >= T) return;
-    const int half = rotary / 2;
-    const float *row = nullptr;
-    if (rotary) row = cos_sin + (int64_t)min(max(positions[t], 0), max_positions - 1) * rotary;
-    auto rotated = [&](const __half *x, float (&out)[N]) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int c = lane + 64 * i;
-            const float a = __half2float(x[c]);
-            if (c < rotary) {
-                const bool lower = c < half;
-                const float b = __half2float(x[lower ? c + half : c - half]);
-                const float co = row[lower ? c : c - half], si = row[half + (lower ? c : c - half)];
-                const float m = a * co, n = b * si;
-                out[i] = lower ? m - n : m + n;
-            } else {
-                out[i] = a;
-            }
+    const int r = threadIdx.x;
+    int s = r < TILE && t0 + r < T ? slots[t0 + r] : -1;
+    if ((unsigned)s >= (unsigned)kv.pages << kv.page_shift) s = -1;
+    // tokens of a block are consecutive slots, and blocks begin at multiples of 32
+    auto at = [&](int v, int k) { const int o = __shfl(v, (r + k) & 63); return r + k >= 0 && r + k < TILE ? o : -1; };
+    const bool four = s >= 0 && s % 4 == 0 && at(s, 1) == s + 1 && at(s, 2) == s + 2 && at(s, 3) == s + 3;
+    auto four_at = [&](int k) { const int o = at(s, k), f = at(four, k); return f == 1 && o == s + k; };
+    const bool g8 = four_at(8), g16 = four_at(16), g24 = four_at(24);
+    const bool whole = ELEM == 2 ? four && s % 16 < 8 && g8 : four && s % 32 < 8 && g8 && g16 && g24;
+    // part of a piece that begins further up
+    const bool inside = s >= 0 && s % 4 && at(four, -(s & 3)) == 1 && at(s, -(s & 3)) == s - (s & 3);
+    const int up = ELEM == 2 ? s & 8 : s & 24;
+    const bool inside_whole = four && up && at(whole, -up) == 1 && at(s, -up) == s - up;
+    const int kind = s < 0 || inside || inside_whole ? 0 : whole ? WHOLE : four ? FOUR : ONE;
+    const uint64_t have = __ballot(kind != 0);
+    if (r < TILE) {
+        p.slot[r] = s;
+        if (kind) {
+            const int n = __popcll(have & ((1ull << r) - 1));
+            p.row[n] = r, p.kind[n] = kind;
         }
-    };
-    if ((int)blockIdx.y < q_heads) {
-        const int64_t at = (int64_t)blockIdx.y * D;
-        float x[N];
-        rotated(q + t * ldq + at, x);
-#pragma unroll
-        for (int i = 0; i < N; ++i) q_out[t * ldqo + at + lane + 64 * i] = __float2half(x[i]);
-        return;
-    }
-    const int h = blockIdx.y - q_heads, slot = slots[t];
-    if ((unsigned)slot >= (unsigned)kv.pages << kv.page_shift) return;
-    float x[N], y[N];
-    rotated(k + t * ldk + (int64_t)h * D, x);
-    bool fine = true;
-    float kmax = 0, vmax = 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        y[i] = __half2float(v[t * ldv + (int64_t)h * D + lane + 64 * i]);
-        if (ELEM == 2) x[i] = __half2float(__float2half(x[i]));
-        fine = fine && finite(x[i]) && finite(y[i]);
-        kmax = fmaxf(kmax, __builtin_fabsf(x[i])), vmax = fmaxf(vmax, __builtin_fabsf(y[i]));
-    }
-    fine = __all(fine);
-    const int rest = slot & (kv.page_size() - 1), token = rest % KV_BLOCK;
-    char *block = kv.block(slot >> kv.page_shift, h, rest);
-    if (ELEM == 2) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int c = lane + 64 * i;
-            *reinterpret_cast<__half *>(block + kv_key_offset<2>(token, c)) = fine ? __float2half(x[i]) : __ushort_as_half(0x7e00);
-            *reinterpret_cast<__half *>(block + kv_value_offset<2>(token, c, D)) = fine ? __float2half(y[i]) : __ushort_as_half(0);
-        }
-        return;
-    }
-    kmax = wave_max(kmax), vmax = wave_max(vmax);
-    const bool some_k = fine && kmax >= KV_NOTHING, some_v = fine && vmax >= KV_NOTHING;
-    const float inv_k = 127.0f / kmax, inv_v = 127.0f / vmax;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int c = lane + 64 * i;
-        const float ck = some_k ? fminf(fmaxf(rintf(x[i] * inv_k), -127.f), 127.f) : 0.f;
-        const float cv = some_v ? fminf(fmaxf(rintf(y[i] * inv_v), -127.f), 127.f) : 0.f;
-        *reinterpret_cast<uint8_t *>(block + kv_key_offset<1>(token, c)) = (uint8_t)((int)ck + 128);
-        *reinterpret_cast<uint8_t *>(block + kv_value_offset<1>(token, c, D)) = (uint8_t)((int)cv + 128);
-    }
-    if (lane < 4) {
-        const float sk = !fine ? __builtin_nanf("") : some_k ? kmax / 127.0f : 0x1p-31f, sv = some_v ? vmax / 127.0f : 0x1p-31f;
-        const float out = lane == 0 ? sk : lane == 1 ? sv : lane == 2 ? log2f(sv) : 1.0f / sv;
-        reinterpret_cast<float *>(block + kv_scale_offset(D))[lane * KV_BLOCK + token] = out;
+        if (r == 0) p.count = __popcll(have);
     }
 }
 
-// One wavefront per token and head.
-template <int ELEM, int D>
-__global__ __launch_bounds__(256) void kv_read_kernel(KvView kv, const int32_t *__restrict__ slots, int T, __half *__restrict__ k, int64_t ldk,
-                                                      __half *__restrict__ v, int64_t ldv)
+// Rotation of 16 channels of a row: the thread's two runs of 8, (8 j, 8 j + half) among the channels that are turned, neighbours among
+// the others.
+struct Turn {
+    int c0, c1;
+    bool turned;
+    __device__ Turn(int j, int rotary) : c0(8 * j), c1(8 * j + rotary / 2), turned(8 * j < rotary / 2)
+    {
+        if (!turned) c0 = rotary + 16 * (j - rotary / 16), c1 = c0 + 8;
+    }
+};
+__device__ inline void widen8(const uint4 &v, float (&f)[8])
 {
-    const int lane = threadIdx.x & 63, t = blockIdx.x * 4 + (threadIdx.x >> 6), h = blockIdx.y;
-    if (t >= T) return;
-    const int slot = slots[t];
-    const bool there = (unsigned)slot < (unsigned)kv.pages << kv.page_shift;
-    const int rest = there ? slot & (kv.page_size() - 1) : 0, token = rest % KV_BLOCK;
-    const char *block = kv.block(there ? slot >> kv.page_shift : 0, h, rest);
+    const unsigned w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) {
-        const int c = lane + 64 * i;
-        float a = 0, b = 0;
-        if (there) {
-            const char *pk = block + kv_key_offset<ELEM>(token, c), *pv = block + kv_value_offset<ELEM>(token, c, D);
-            if (ELEM == 2) {
-                a = __half2float(*reinterpret_cast<const __half *>(pk)), b = __half2float(*reinterpret_cast<const __half *>(pv));
-            } else {
-                const float *s = reinterpret_cast<const float *>(block + kv_scale_offset(D));
-                a = (float)(*reinterpret_cast<const uint8_t *>(pk) - 128) * s[token];
-                b = (float)(*reinterpret_cast<const uint8_t *>(pv) - 128) * s[KV_BLOCK + token];
+    for (int i = 0; i < 4; ++i) f[2 * i] = half_bits_to_float(w[i] & 0xffffu), f[2 * i + 1] = half_bits_to_float(w[i] >> 16);
+}
+__device__ inline uint4 narrow8(const float (&f)[8])
+{
+    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+    unsigned w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __builtin_bit_cast(unsigned, h2{(_Float16)f[2 * i], (_Float16)f[2 * i + 1]});
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ inline void rotate(const Turn &u, const float *row, int rotary, float (&a)[8], float (&b)[8])
+{
+    if (!u.turned) return;
+    const float4 c0 = *reinterpret_cast<const float4 *>(row + u.c0), c1 = *reinterpret_cast<const float4 *>(row + u.c0 + 4);
+    const float4 s0 = *reinterpret_cast<const float4 *>(row + rotary / 2 + u.c0), s1 = *reinterpret_cast<const float4 *>(row + rotary / 2 + u.c0 + 4);
+    const float co[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w}, si[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {                         // (no contraction: each product and each sum is rounded)
+        const float x = a[i], y = b[i];
+        a[i] = x * co[i] - y * si[i];
+        b[i] = y * co[i] + x * si[i];
+    }
+}
+__device__ inline uint2 codes8(const float (&f)[8], float inv, bool some)
+{
+    unsigned w[2] = {0x80808080u, 0x80808080u};           // codes are stored plus 128
+    if (some) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int q = (int)fminf(fmaxf(rintf(f[i] * inv), -127.f), 127.f);
+            w[i / 4] ^= (unsigned)(q & 255) << (8 * (i % 4));   // q + 128 = q ^ 128 in a byte
+        }
+    }
+    return make_uint2(w[0], w[1]);
+}
+
+__device__ inline uint4 kept(const uint4 &v, bool keep, unsigned other) { return make_uint4(keep ? v.x : other, keep ? v.y : other, keep ? v.z : other, keep ? v.w : other); }
+
+struct AppendArgs {
+    const __half *q, *k, *v;
+    int64_t ldq, ldk, ldv, ldqo;
+    __half *q_out;
+    const float *cos_sin;
+    const int32_t *positions, *slots;
+    int T, q_heads, rotary, max_positions, kv_groups;     // kv_groups: workgroups of keys and values (the first ones of the grid)
+    KvView kv;
+};
+
+template <int ELEM, int D>
+__global__ __launch_bounds__(2 * D) void kv_append_kernel(AppendArgs a)
+{
+    constexpr int LANES = D / 16, ROW = ELEM * D + 16;    // lanes of a token; bytes of a row of values in LDS
+    const int tid = threadIdx.x;
+    auto table_row = [&](int t) { return a.cos_sin + (int64_t)min(max(a.positions[t], 0), a.max_positions - 1) * a.rotary; };
+
+    if ((int)blockIdx.x >= a.kv_groups) {                 // queries: 32 (token, head) pairs
+        const int64_t pair = (int64_t)(blockIdx.x - a.kv_groups) * TILE + tid / LANES;
+        const int t = (int)(pair / a.q_heads), head = (int)(pair % a.q_heads);
+        if (t >= a.T) return;
+        const Turn u(tid % LANES, a.rotary);
+        const __half *src = a.q + t * a.ldq + (int64_t)head * D;
+        __half *dst = a.q_out + t * a.ldqo + (int64_t)head * D;
+        uint4 lo = *reinterpret_cast<const uint4 *>(src + u.c0), hi = *reinterpret_cast<const uint4 *>(src + u.c1);
+        if (u.turned) {
+            float x[8], y[8];
+            widen8(lo, x), widen8(hi, y);
+            rotate(u, table_row(t), a.rotary, x, y);
+            lo = narrow8(x), hi = narrow8(y);
+        }
+        *reinterpret_cast<uint4 *>(dst + u.c0) = lo;
+        *reinterpret_cast<uint4 *>(dst + u.c1) = hi;
+        return;
+    }
+
+    __shared__ Pieces p;
+    __shared__ __attribute__((aligned(16))) char values[TILE * ROW];
+    const int head = blockIdx.x % a.kv.heads, t0 = blockIdx.x / a.kv.heads * TILE;
+    const int r = tid / LANES, j = tid % LANES, t = min(t0 + r, a.T - 1);     // (a row behind the last one: the last one again, stored nowhere)
+    const Turn u(j, a.rotary);
+    const __half *ks = a.k + t * a.ldk + (int64_t)head * D, *vs = a.v + t * a.ldv + (int64_t)head * D + 16 * j;
+    const uint4 k0 = *reinterpret_cast<const uint4 *>(ks + u.c0), k1 = *reinterpret_cast<const uint4 *>(ks + u.c1);
+    const uint4 v0 = *reinterpret_cast<const uint4 *>(vs), v1 = *reinterpret_cast<const uint4 *>(vs + 8);
+    if (tid < 64) find_pieces<ELEM>(p, a.slots, t0, a.T, a.kv);
+    float x[8], y[8], z[8], w[8];
+    widen8(k0, x), widen8(k1, y), widen8(v0, z), widen8(v1, w);
+    if (a.rotary) rotate(u, table_row(t), a.rotary, x, y);
+    uint4 kh0, kh1;
+    if (ELEM == 2) {
+        kh0 = narrow8(x), kh1 = narrow8(y);
+        widen8(kh0, x), widen8(kh1, y);
+    }
+    float kmax = 0, vmax = 0, off = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (!(finite(x[i]) && finite(y[i]) && finite(z[i]) && finite(w[i]))) off = 1;
+        kmax = fmaxf(kmax, fmaxf(__builtin_fabsf(x[i]), __builtin_fabsf(y[i]))), vmax = fmaxf(vmax, fmaxf(__builtin_fabsf(z[i]), __builtin_fabsf(w[i])));
+    }
+    auto most = [](float a, float b) { return fmaxf(a, b); };
+    const bool fine = over_lanes<LANES>(off, most) == 0;
+    __syncthreads();                                      // pieces are there
+    const int slot = p.slot[r], rest = slot & (a.kv.page_size() - 1), token = rest % KV_BLOCK;
+    char *block = slot < 0 ? nullptr : a.kv.block(slot >> a.kv.page_shift, head, rest);
+    char *mine = values + r * ROW + 16 * j * ELEM;
+    if constexpr (ELEM == 2) {
+        if (slot >= 0) {
+            *reinterpret_cast<uint4 *>(block + kv_key_offset<2>(token, u.c0)) = kept(kh0, fine, 0x7e007e00u);
+            *reinterpret_cast<uint4 *>(block + kv_key_offset<2>(token, u.c1)) = kept(kh1, fine, 0x7e007e00u);
+        }
+        *reinterpret_cast<uint4 *>(mine) = kept(v0, fine, 0);
+        *reinterpret_cast<uint4 *>(mine + 16) = kept(v1, fine, 0);
+    } else {
+        kmax = over_lanes<LANES>(kmax, most), vmax = over_lanes<LANES>(vmax, most);
+        const bool some_k = fine && kmax >= KV_NOTHING, some_v = fine && vmax >= KV_NOTHING;
+        const float inv_k = 127.0f / kmax, inv_v = 127.0f / vmax;
+        const uint2 q0 = codes8(x, inv_k, some_k), q1 = codes8(y, inv_k, some_k), c0 = codes8(z, inv_v, some_v), c1 = codes8(w, inv_v, some_v);
+        if (slot >= 0) {
+            *reinterpret_cast<uint2 *>(block + kv_key_offset<1>(token, u.c0)) = q0;
+            *reinterpret_cast<uint2 *>(block + kv_key_offset<1>(token, u.c1)) = q1;
+            if (j < 4) {
+                const float sk = !fine ? __builtin_nanf("") : some_k ? kmax / 127.0f : 0x1p-31f, sv = some_v ? vmax / 127.0f : 0x1p-31f;
+                const float out = j == 0 ? sk : j == 1 ? sv : j == 2 ? log2f(sv) : 1.0f / sv;
+                reinterpret_cast<float *>(block + kv_scale_offset(D))[j * KV_BLOCK + token] = out;
             }
         }
-        if (k) k[t * ldk + (int64_t)h * D + c] = __float2half(a);
-        if (v) v[t * ldv + (int64_t)h * D + c] = __float2half(b);
+        *reinterpret_cast<uint4 *>(mine) = make_uint4(c0.x, c0.y, c1.x, c1.y);
     }
+    __syncthreads();
+    const int c = tid % D;                                // a channel per thread, every second piece
+    for (int i = tid / D; i < p.count; i += 2) {
+        const int row = p.row[i], kind = p.kind[i], s = p.slot[row], in_page = s & (a.kv.page_size() - 1);
+        char *to = a.kv.block(s >> a.kv.page_shift, head, in_page) + kv_value_offset<ELEM>(in_page % KV_BLOCK, c, D);
+        if constexpr (ELEM == 2) {
+            auto two = [&](int k) {
+                const char *from = values + (row + k) * ROW + 2 * c;
+                return (unsigned)*reinterpret_cast<const uint16_t *>(from) | (unsigned)*reinterpret_cast<const uint16_t *>(from + ROW) << 16;
+            };
+            if (kind == WHOLE) *reinterpret_cast<uint4 *>(to) = make_uint4(two(0), two(2), two(8), two(10));
+            else if (kind == FOUR) *reinterpret_cast<uint2 *>(to) = make_uint2(two(0), two(2));
+            else *reinterpret_cast<uint16_t *>(to) = (uint16_t)two(0);
+        } else {
+            auto four = [&](int k) {
+                const uint8_t *from = reinterpret_cast<const uint8_t *>(values) + (row + k) * ROW + c;
+                return (unsigned)from[0] | (unsigned)from[ROW] << 8 | (unsigned)from[2 * ROW] << 16 | (unsigned)from[3 * ROW] << 24;
+            };
+            if (kind == WHOLE) *reinterpret_cast<uint4 *>(to) = make_uint4(four(0), four(8), four(16), four(24));
+            else if (kind == FOUR) *reinterpret_cast<unsigned *>(to) = four(0);
+            else *reinterpret_cast<uint8_t *>(to) = *(reinterpret_cast<const uint8_t *>(values) + row * ROW + c);
+        }
+    }
+}
+
+template <int ELEM, int D>
+__global__ __launch_bounds__(2 * D) void kv_read_kernel(KvView kv, const int32_t *__restrict__ slots, int T, __half *__restrict__ k, int64_t ldk,
+                                                        __half *__restrict__ v, int64_t ldv)
+{
+    constexpr int LANES = D / 16, ROW = ELEM * D + 16;
+    __shared__ Pieces p;
+    __shared__ __attribute__((aligned(16))) char values[TILE * ROW];
+    const int tid = threadIdx.x, head = blockIdx.x % kv.heads, t0 = blockIdx.x / kv.heads * TILE;
+    if (tid < 64) find_pieces<ELEM>(p, slots, t0, T, kv);
+    __syncthreads();
+    const int c = tid % D;
+    if (v) {
+        for (int i = tid / D; i < p.count; i += 2) {
+            const int row = p.row[i], kind = p.kind[i], s = p.slot[row], in_page = s & (kv.page_size() - 1);
+            const char *from = kv.block(s >> kv.page_shift, head, in_page) + kv_value_offset<ELEM>(in_page % KV_BLOCK, c, D);
+            if constexpr (ELEM == 2) {
+                auto put = [&](int k, unsigned w) {
+                    char *to = values + (row + k) * ROW + 2 * c;
+                    *reinterpret_cast<uint16_t *>(to) = (uint16_t)w, *reinterpret_cast<uint16_t *>(to + ROW) = (uint16_t)(w >> 16);
+                };
+                if (kind == WHOLE) {
+                    const uint4 w = *reinterpret_cast<const uint4 *>(from);
+                    put(0, w.x), put(2, w.y), put(8, w.z), put(10, w.w);
+                } else if (kind == FOUR) {
+                    const uint2 w = *reinterpret_cast<const uint2 *>(from);
+                    put(0, w.x), put(2, w.y);
+                } else {
+                    *reinterpret_cast<uint16_t *>(values + row * ROW + 2 * c) = *reinterpret_cast<const uint16_t *>(from);
+                }
+            } else {
+                auto put = [&](int k, unsigned w) {
+                    uint8_t *to = reinterpret_cast<uint8_t *>(values) + (row + k) * ROW + c;
+                    to[0] = (uint8_t)w, to[ROW] = (uint8_t)(w >> 8), to[2 * ROW] = (uint8_t)(w >> 16), to[3 * ROW] = (uint8_t)(w >> 24);
+                };
+                if (kind == WHOLE) {
+                    const uint4 w = *reinterpret_cast<const uint4 *>(from);
+                    put(0, w.x), put(8, w.y), put(16, w.z), put(24, w.w);
+                } else if (kind == FOUR) {
+                    put(0, *reinterpret_cast<const unsigned *>(from));
+                } else {
+                    *(reinterpret_cast<uint8_t *>(values) + row * ROW + c) = *reinterpret_cast<const uint8_t *>(from);
+                }
+            }
+        }
+        __syncthreads();
+    }
+    const int r = tid / LANES, j = tid % LANES, t = t0 + r;
+    if (t >= T) return;
+    const int slot = p.slot[r], rest = slot & (kv.page_size() - 1), token = rest % KV_BLOCK;
+    const char *block = slot < 0 ? nullptr : kv.block(slot >> kv.page_shift, head, rest);
+    float sk = 0, sv = 0;
+    if (ELEM == 1 && slot >= 0) {
+        const float *s = reinterpret_cast<const float *>(block + kv_scale_offset(D));
+        sk = s[token], sv = s[KV_BLOCK + token];
+    }
+    auto scaled = [&](uint2 w, float s) {
+        float f[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = (float)((int)((i < 4 ? w.x : w.y) >> (8 * (i % 4)) & 255u) - 128) * s;
+        return narrow8(f);
+    };
+    const uint4 none = make_uint4(0, 0, 0, 0);
+    auto store = [&](__half *to, int64_t ld, const char *piece, int second, float s) {   // 16 channels; fp16: in two runs of 8
+        uint4 a = none, b = none;
+        if (slot >= 0) {
+            if constexpr (ELEM == 2) {
+                a = *reinterpret_cast<const uint4 *>(piece), b = *reinterpret_cast<const uint4 *>(piece + second);
+            } else {
+                const uint4 w = *reinterpret_cast<const uint4 *>(piece);
+                a = scaled(make_uint2(w.x, w.y), s), b = scaled(make_uint2(w.z, w.w), s);
+            }
+        }
+        __half *dst = to + t * ld + (int64_t)head * D + 16 * j;
+        *reinterpret_cast<uint4 *>(dst) = a, *reinterpret_cast<uint4 *>(dst + 8) = b;
+    };
+    if (k) store(k, ldk, slot < 0 ? nullptr : block + kv_key_offset<ELEM>(token, 16 * j), 512, sk);
+    if (v) store(v, ldv, values + r * ROW + 16 * j * ELEM, 16, sv);
 }
 
 __global__ void kv_no_requests_kernel(const int32_t *pool, int32_t *pool_out, int32_t *cu_new)
@@ -311,8 +497,10 @@ int launch_kv_append(const __half *q, int64_t ldq, const __half *k, int64_t ldk,
                      const float *cos_sin, int rotary, int max_positions, const int32_t *positions, const int32_t *slots,
                      __half *q_out, int64_t ldqo, const KvView &kv, hipStream_t st)
 {
-    const dim3 grid(ceil_div(T, 4), q_heads + kv.heads);
-#define QL_CALL(E, D) kv_append_kernel<E, D><<<grid, 256, 0, st>>>(q, ldq, k, ldk, v, ldv, T, q_heads, cos_sin, rotary, max_positions, positions, slots, q_out, ldqo, kv)
+    const int64_t pairs = (int64_t)T * q_heads, kv_groups = (int64_t)ceil_div(T, TILE) * kv.heads, grid = kv_groups + (pairs + TILE - 1) / TILE;
+    if (grid >= (int64_t)1 << 31) return fail(QL_ERR_UNSUPPORTED, "%d tokens of %d and %d heads are more than a launch holds", T, q_heads, kv.heads);
+    const AppendArgs a = {q, k, v, ldq, ldk, ldv, ldqo, q_out, cos_sin, positions, slots, T, q_heads, rotary, max_positions, (int)kv_groups, kv};
+#define QL_CALL(E, D) kv_append_kernel<E, D><<<(unsigned)grid, 2 * D, 0, st>>>(a)
     QL_KV_DISPATCH(kv, QL_CALL);
 #undef QL_CALL
     return check_hip(hipGetLastError(), "kv_append_kernel");
@@ -320,8 +508,9 @@ int launch_kv_append(const __half *q, int64_t ldq, const __half *k, int64_t ldk,
 
 int launch_kv_read(const KvView &kv, const int32_t *slots, int T, __half *k, int64_t ldk, __half *v, int64_t ldv, hipStream_t st)
 {
-    const dim3 grid(ceil_div(T, 4), kv.heads);
-#define QL_CALL(E, D) kv_read_kernel<E, D><<<grid, 256, 0, st>>>(kv, slots, T, k, ldk, v, ldv)
+    const int64_t grid = (int64_t)ceil_div(T, TILE) * kv.heads;
+    if (grid >= (int64_t)1 << 31) return fail(QL_ERR_UNSUPPORTED, "%d tokens of %d heads are more than a launch holds", T, kv.heads);
+#define QL_CALL(E, D) kv_read_kernel<E, D><<<(unsigned)grid, 2 * D, 0, st>>>(kv, slots, T, k, ldk, v, ldv)
     QL_KV_DISPATCH(kv, QL_CALL);
 #undef QL_CALL
     return check_hip(hipGetLastError(), "kv_read_kernel");

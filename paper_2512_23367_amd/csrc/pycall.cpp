@@ -8,6 +8,8 @@
 // well, and nothing is reported from here.  One token through 1536 x 1536: 6.1 us a call through ctypes, 4.0 here.
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/TensorSubclassLikeUtils.h>
+#include <c10/core/impl/DeviceGuardImplInterface.h>
+#include <algorithm>
 #include <climits>
 #include <cstdint>
 #include <cstring>
@@ -27,7 +29,14 @@ struct Library {
     decltype(&ql_quant_act_rmsnorm) quant_rmsnorm;
     decltype(&ql_quant_act_swiglu) quant_swiglu;
     decltype(&ql_quant_act_per_token_transformed) quant_transformed;
+    decltype(&ql_kv_cache_bytes) kv_cache_bytes;
+    decltype(&ql_kv_resize) kv_resize;
+    decltype(&ql_kv_append) kv_append;
+    decltype(&ql_kv_read) kv_read;
+    decltype(&ql_paged_attention) paged_attention;
 } lib;
+
+PyObject *format_type = nullptr;   // binding.py's QlKvFormat
 
 // An argument that is not in order: the caller returns None.
 struct NotPlain {};
@@ -277,6 +286,183 @@ PyObject *quant_transformed(PyObject *, Args a, Py_ssize_t n)   // x, inv_smooth
     });
 }
 
+// ---- the paged cache: what its calls take, checked as binding.py checks it; tensors have to be of the current device ----
+
+struct Here {
+    c10::DeviceIndex index = c10::impl::getDeviceGuardImpl(c10::DeviceType::CUDA)->getDevice().index();
+    const at::Tensor &operator()(PyObject *o) const
+    {
+        const at::Tensor &t = tensor(o);
+        if (t.get_device() != index) throw NotPlain();
+        return t;
+    }
+    int32_t *ints(PyObject *o, int64_t n) const
+    {
+        const at::Tensor &t = (*this)(o);
+        if (t.scalar_type() != at::kInt || t.numel() < n || !t.is_contiguous()) throw NotPlain();
+        return static_cast<int32_t *>(t.data_ptr());
+    }
+};
+
+struct Format {
+    ql_kv_format f;
+    explicit Format(PyObject *o)
+    {
+        if (!format_type || (PyObject *)Py_TYPE(o) != format_type) throw NotPlain();
+        Py_buffer b;
+        if (PyObject_GetBuffer(o, &b, PyBUF_SIMPLE) != 0) throw NotPlain();
+        const bool fits = b.len == (Py_ssize_t)sizeof(f);
+        if (fits) memcpy(&f, b.buf, sizeof(f));
+        PyBuffer_Release(&b);
+        if (!fits || f.head_dim < 1) throw NotPlain();
+    }
+};
+
+// fp16 [rows, heads * head_dim] with unit inner stride
+struct Rows {
+    void *p = nullptr;
+    int rows = 0, heads = 0;
+    int64_t ld = 0;
+    Rows() {}
+    Rows(const Here &here, PyObject *o, int head_dim)
+    {
+        const at::Tensor &t = here(o);
+        if (t.scalar_type() != at::kHalf || t.dim() != 2 || t.size(0) < 1 || t.stride(1) != 1 || t.size(1) % head_dim) throw NotPlain();
+        p = t.data_ptr(), rows = as_int(t.size(0)), heads = as_int(t.size(1) / head_dim);
+        ld = rows > 1 ? t.stride(0) : (t.size(1) + 7) / 8 * 8;
+    }
+    const Rows &fit(int r, int h) const
+    {
+        if (rows != r || heads != h) throw NotPlain();
+        return *this;
+    }
+};
+
+struct Table {
+    int32_t *p;
+    int64_t ld;
+    int columns;
+    Table(const Here &here, PyObject *o, int64_t requests)
+    {
+        const at::Tensor &t = here(o);
+        if (t.scalar_type() != at::kInt || t.dim() != 2 || t.size(0) < requests || t.size(0) < 1 || t.stride(1) != 1) throw NotPlain();
+        p = static_cast<int32_t *>(t.data_ptr()), columns = as_int(t.size(1)), ld = t.size(0) > 1 ? t.stride(0) : t.size(1);
+    }
+};
+
+void *cache_of(const Here &here, PyObject *o, const ql_kv_format &f)
+{
+    size_t need = 0;
+    const at::Tensor &t = here(o);
+    if (lib.kv_cache_bytes(&f, &need) != QL_OK || !t.is_contiguous() || t.nbytes() < need) throw NotPlain();
+    return t.data_ptr();
+}
+
+int as_flag(PyObject *o)
+{
+    if (o == Py_True) return 1;
+    if (o == Py_False) return 0;
+    throw NotPlain();
+}
+
+// page_size, old_len, want_len, ring, pool, pool_out, block_table, kv_len, cu_new, slots, positions, stream
+PyObject *kv_resize(PyObject *, Args a, Py_ssize_t n)
+{
+    return call(n, 12, [&] {
+        const Here here;
+        const int page = as_int(a[0]), requests = as_int(here(a[1]).numel()), pages = as_int(here(a[3]).numel());
+        const int most = as_int(std::min(here(a[9]).numel(), here(a[10]).numel()));
+        const int32_t *old_len = here.ints(a[1], requests), *want = here.ints(a[2], requests), *pool = here.ints(a[4], 4);
+        int32_t *ring = here.ints(a[3], 1), *pool_out = here.ints(a[5], 4), *kv_len = here.ints(a[7], requests);
+        int32_t *cu = here.ints(a[8], (int64_t)requests + 1), *slots = here.ints(a[9], most), *positions = here.ints(a[10], most);
+        const Table t(here, a[6], requests);
+        void *st = stream_from(a[11]);
+        return [=] {
+            return lib.kv_resize(old_len, want, requests, page, ring, pages, pool, pool_out, t.p, t.ld, t.columns, kv_len, cu, slots, positions, most, st);
+        };
+    });
+}
+
+PyObject *kv_append(PyObject *, Args a, Py_ssize_t n)   // q, k, v, cos_sin, positions, slots, q_out, cache, fmt, stream
+{
+    return call(n, 10, [&] {
+        const Here here;
+        const Format f(a[8]);
+        const Rows k(here, a[1], f.f.head_dim), v(here, a[2], f.f.head_dim);
+        const int T = k.rows;
+        k.fit(T, f.f.heads), v.fit(T, f.f.heads);
+        const float *cs = nullptr;
+        const int32_t *positions = nullptr, *slots = here.ints(a[5], T);
+        int rotary = 0, most = 0;
+        if (a[3] != Py_None) {
+            const at::Tensor &t = here(a[3]);
+            if (t.scalar_type() != at::kFloat || t.dim() != 2 || !t.is_contiguous()) throw NotPlain();
+            cs = static_cast<const float *>(t.data_ptr()), most = as_int(t.size(0)), rotary = as_int(t.size(1)), positions = here.ints(a[4], T);
+        }
+        Rows q, out;
+        if (a[0] != Py_None) {
+            q = Rows(here, a[0], f.f.head_dim), out = Rows(here, a[6], f.f.head_dim);
+            q.fit(T, q.heads), out.fit(T, q.heads);
+        } else if (a[6] != Py_None) {
+            throw NotPlain();
+        }
+        void *cache = cache_of(here, a[7], f.f), *st = stream_from(a[9]);
+        return [=] {
+            return lib.kv_append(q.p, q.ld, k.p, k.ld, v.p, v.ld, T, q.heads, cs, rotary, most, positions, slots, out.p, out.ld, cache, &f.f, st);
+        };
+    });
+}
+
+PyObject *kv_read(PyObject *, Args a, Py_ssize_t n)   // cache, fmt, slots, k, v, stream
+{
+    return call(n, 6, [&] {
+        const Here here;
+        const Format f(a[1]);
+        Rows k, v;
+        if (a[3] != Py_None) k = Rows(here, a[3], f.f.head_dim);
+        if (a[4] != Py_None) v = Rows(here, a[4], f.f.head_dim);
+        if (!k.p && !v.p) throw NotPlain();
+        const int T = k.p ? k.rows : v.rows;
+        if (k.p) k.fit(T, f.f.heads);
+        if (v.p) v.fit(T, f.f.heads);
+        const int32_t *slots = here.ints(a[2], T);
+        void *cache = cache_of(here, a[0], f.f), *st = stream_from(a[5]);
+        return [=] { return lib.kv_read(cache, &f.f, slots, T, k.p, k.ld, v.p, v.ld, st); };
+    });
+}
+
+// q, cache, fmt, block_table, cu_new, ctx_len, kv_len, scale, y, ws, causal, window, max_new, stream
+PyObject *paged_attention(PyObject *, Args a, Py_ssize_t n)
+{
+    return call(n, 14, [&] {
+        const Here here;
+        const Format f(a[2]);
+        const Rows q(here, a[0], f.f.head_dim), y(here, a[8], f.f.head_dim);
+        y.fit(q.rows, q.heads);
+        const int requests = as_int(here(a[6]).numel());
+        const Table t(here, a[3], requests);
+        const int32_t *cu = here.ints(a[4], (int64_t)requests + 1), *ctx = a[5] == Py_None ? nullptr : here.ints(a[5], requests), *len = here.ints(a[6], requests);
+        const float scale = as_float(a[7]);
+        void *ws = nullptr;
+        size_t bytes = 0;
+        if (a[9] != Py_None) ws = here(a[9]).data_ptr(), bytes = tensor(a[9]).nbytes();
+        const int causal = as_flag(a[10]), window = as_int(a[11]), most = as_int(a[12]);
+        void *cache = cache_of(here, a[1], f.f), *st = stream_from(a[13]);
+        return [=] {
+            return lib.paged_attention(q.p, q.ld, q.rows, q.heads, cache, &f.f, t.p, t.ld, t.columns, cu, ctx, len, requests, scale, causal, window, most, y.p, y.ld,
+                                       ws, bytes, st);
+        };
+    });
+}
+
+// bind_format(type): the class of binding.py that mirrors ql_kv_format
+PyObject *bind_format(PyObject *, PyObject *type)
+{
+    Py_INCREF(type);
+    Py_XSETREF(format_type, type);
+    Py_RETURN_NONE;
+}
+
 // bind(addresses): the entry points of the library that binding.py has loaded, in the order of struct Library
 PyObject *bind(PyObject *, PyObject *addresses)
 {
@@ -297,8 +483,8 @@ PyObject *bind(PyObject *, PyObject *addresses)
 
 #define QL_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {QL_METHOD(w8a8_linear), QL_METHOD(w4a8_linear), QL_METHOD(w8a8_gemm), QL_METHOD(w4a8_gemm), QL_METHOD(quant_act),
-                         QL_METHOD(quant_rmsnorm), QL_METHOD(quant_swiglu), QL_METHOD(quant_transformed),
-                         {"bind", bind, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         QL_METHOD(quant_rmsnorm), QL_METHOD(quant_swiglu), QL_METHOD(quant_transformed), QL_METHOD(kv_resize), QL_METHOD(kv_append), QL_METHOD(kv_read),
+                         QL_METHOD(paged_attention), {"bind_format", bind_format, METH_O, nullptr}, {"bind", bind, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_qlcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

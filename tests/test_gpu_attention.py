@@ -188,3 +188,14 @@ def test_refusals_of_the_binding(U):
     with pytest.raises(ql.QlError) as e:
         ql.ql_paged_attention(q, r.cache, r.fmt, U.ints(r.table), U.ints(r.cu), None, U.ints(r.len), 1.0, y)
     assert e.value.status == 1
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("requests,new_most,max_new", [(63, 1, 1), (64, 3, 3), (65, 1, 1), (130, 60, 0), (300, 2, 2), (700, 1, 1)])
+def test_many_requests(U, requests, new_most, max_new, bits):
+    """Around and beyond a wavefront's and a workgroup's number of requests, one of them long, some with nothing to do."""
+    rng = np.random.default_rng(requests)
+    ctx, new = rng.integers(0, 90, requests), rng.integers(0, new_most + 1, requests)
+    ctx[requests // 2], new[requests // 2], ctx[-1], new[-1] = 3000, 1, 700, new_most
+    r = U.Requests(requests, ctx.tolist(), new.tolist(), 4, 2, 64, bits, 32)
+    r.check(r.call(max_new=max_new), rows=np.unique(np.r_[rng.integers(0, r.T, 60), r.T - 1, r.cu[requests // 2]]))
