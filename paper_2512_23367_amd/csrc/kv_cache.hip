@@ -157,7 +157,6 @@ __global__ __launch_bounds__(RESIZE_THREADS) void kv_resize_kernel(const int32_t
 // a block: they go through LDS, and leave (arrive) 16 bytes at a time where the rows fill the piece of a channel -- 8 tokens in fp16, 16 in
 // int8 --, else by groups of 4 tokens, else singly: a decode step's tokens are single ones, a prompt's rows have them at its ends only.
 // 4096 tokens, 32 + 2 x 32 heads of 128, fp16, and 16001 tokens, 32 + 2 x 8 heads, int8; append / read back, us:  APPEND_FIGURES
-constexpr int TILE = 32;
 
 __device__ inline bool finite(float x) { return __builtin_fabsf(x) <= 3.402823466e38f; }
 
@@ -178,14 +177,15 @@ __device__ inline float over_lanes(float v, OP op)
 
 // How the 32 rows' values lie in their blocks: pieces to move, {row of the first token, kind}.
 enum { ONE = 1, FOUR = 2, WHOLE = 3 };
+template <int TILE>
 struct Pieces {
     int slot[TILE];                                       // -1: none
     int count, row[TILE], kind[TILE];
 };
 
 // by the first wavefront
-template <int ELEM>
-__device__ inline void find_pieces(Pieces &p, const int32_t *slots, int t0, int T, const KvView &kv)
+template <int ELEM, int TILE>
+__device__ inline void find_pieces(Pieces<TILE> &p, const int32_t *slots, int t0, int T, const KvView &kv)
 {
     const int r = threadIdx.x;
     int s = r < TILE && t0 + r < T ? slots[t0 + r] : -1;
@@ -274,15 +274,15 @@ struct AppendArgs {
     KvView kv;
 };
 
-template <int ELEM, int D>
+template <int ELEM, int D, int TILE>
 __global__ __launch_bounds__(2 * D) void kv_append_kernel(AppendArgs a)
 {
-    constexpr int LANES = D / 16, ROW = ELEM * D + 16;    // lanes of a token; bytes of a row of values in LDS
+    constexpr int LANES = D / 16, ROW = ELEM * D + 16;    // lanes of a token; bytes of a row in LDS
     const int tid = threadIdx.x;
     auto table_row = [&](int t) { return a.cos_sin + (int64_t)min(max(a.positions[t], 0), a.max_positions - 1) * a.rotary; };
 
     if ((int)blockIdx.x >= a.kv_groups) {                 // queries: 32 (token, head) pairs
-        const int64_t pair = (int64_t)(blockIdx.x - a.kv_groups) * TILE + tid / LANES;
+        const int64_t pair = (int64_t)(blockIdx.x - a.kv_groups) * 32 + tid / LANES;
         const int t = (int)(pair / a.q_heads), head = (int)(pair % a.q_heads);
         if (t >= a.T) return;
         const Turn u(tid % LANES, a.rotary);
@@ -300,60 +300,66 @@ __global__ __launch_bounds__(2 * D) void kv_append_kernel(AppendArgs a)
         return;
     }
 
-    __shared__ Pieces p;
-    __shared__ __attribute__((aligned(16))) char values[TILE * ROW];
+    __shared__ Pieces<TILE> p;
+    __shared__ __attribute__((aligned(16))) char keys[TILE * ROW], values[TILE * ROW];
     const int head = blockIdx.x % a.kv.heads, t0 = blockIdx.x / a.kv.heads * TILE;
-    const int r = tid / LANES, j = tid % LANES, t = min(t0 + r, a.T - 1);     // (a row behind the last one: the last one again, stored nowhere)
-    const Turn u(j, a.rotary);
-    const __half *ks = a.k + t * a.ldk + (int64_t)head * D, *vs = a.v + t * a.ldv + (int64_t)head * D + 16 * j;
-    const uint4 k0 = *reinterpret_cast<const uint4 *>(ks + u.c0), k1 = *reinterpret_cast<const uint4 *>(ks + u.c1);
-    const uint4 v0 = *reinterpret_cast<const uint4 *>(vs), v1 = *reinterpret_cast<const uint4 *>(vs + 8);
-    if (tid < 64) find_pieces<ELEM>(p, a.slots, t0, a.T, a.kv);
-    float x[8], y[8], z[8], w[8];
-    widen8(k0, x), widen8(k1, y), widen8(v0, z), widen8(v1, w);
-    if (a.rotary) rotate(u, table_row(t), a.rotary, x, y);
-    uint4 kh0, kh1;
-    if (ELEM == 2) {
-        kh0 = narrow8(x), kh1 = narrow8(y);
-        widen8(kh0, x), widen8(kh1, y);
-    }
-    float kmax = 0, vmax = 0, off = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if (!(finite(x[i]) && finite(y[i]) && finite(z[i]) && finite(w[i]))) off = 1;
-        kmax = fmaxf(kmax, fmaxf(__builtin_fabsf(x[i]), __builtin_fabsf(y[i]))), vmax = fmaxf(vmax, fmaxf(__builtin_fabsf(z[i]), __builtin_fabsf(w[i])));
-    }
-    auto most = [](float a, float b) { return fmaxf(a, b); };
-    const bool fine = over_lanes<LANES>(off, most) == 0;
-    __syncthreads();                                      // pieces are there
-    const int slot = p.slot[r], rest = slot & (a.kv.page_size() - 1), token = rest % KV_BLOCK;
-    char *block = slot < 0 ? nullptr : a.kv.block(slot >> a.kv.page_shift, head, rest);
-    char *mine = values + r * ROW + 16 * j * ELEM;
-    if constexpr (ELEM == 2) {
-        if (slot >= 0) {
-            *reinterpret_cast<uint4 *>(block + kv_key_offset<2>(token, u.c0)) = kept(kh0, fine, 0x7e007e00u);
-            *reinterpret_cast<uint4 *>(block + kv_key_offset<2>(token, u.c1)) = kept(kh1, fine, 0x7e007e00u);
+    const int r = tid / LANES, j = tid % LANES;
+    if (TILE == 32 || r < TILE) {
+        const int t = min(t0 + r, a.T - 1);               // (a row behind the last one: the last one again, stored nowhere)
+        const Turn u(j, a.rotary);
+        const __half *ks = a.k + t * a.ldk + (int64_t)head * D, *vs = a.v + t * a.ldv + (int64_t)head * D + 16 * j;
+        const uint4 k0 = *reinterpret_cast<const uint4 *>(ks + u.c0), k1 = *reinterpret_cast<const uint4 *>(ks + u.c1);
+        const uint4 v0 = *reinterpret_cast<const uint4 *>(vs), v1 = *reinterpret_cast<const uint4 *>(vs + 8);
+        const int s = t0 + r < a.T ? a.slots[t] : -1;
+        const bool stored = (unsigned)s < (unsigned)a.kv.pages << a.kv.page_shift;
+        float x[8], y[8], z[8], w[8];
+        widen8(k0, x), widen8(k1, y), widen8(v0, z), widen8(v1, w);
+        if (a.rotary) rotate(u, table_row(t), a.rotary, x, y);
+        uint4 kh0, kh1;
+        if (ELEM == 2) {
+            kh0 = narrow8(x), kh1 = narrow8(y);
+            widen8(kh0, x), widen8(kh1, y);
         }
-        *reinterpret_cast<uint4 *>(mine) = kept(v0, fine, 0);
-        *reinterpret_cast<uint4 *>(mine + 16) = kept(v1, fine, 0);
-    } else {
-        kmax = over_lanes<LANES>(kmax, most), vmax = over_lanes<LANES>(vmax, most);
-        const bool some_k = fine && kmax >= KV_NOTHING, some_v = fine && vmax >= KV_NOTHING;
-        const float inv_k = 127.0f / kmax, inv_v = 127.0f / vmax;
-        const uint2 q0 = codes8(x, inv_k, some_k), q1 = codes8(y, inv_k, some_k), c0 = codes8(z, inv_v, some_v), c1 = codes8(w, inv_v, some_v);
-        if (slot >= 0) {
-            *reinterpret_cast<uint2 *>(block + kv_key_offset<1>(token, u.c0)) = q0;
-            *reinterpret_cast<uint2 *>(block + kv_key_offset<1>(token, u.c1)) = q1;
-            if (j < 4) {
+        float kmax = 0, vmax = 0, off = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (!(finite(x[i]) && finite(y[i]) && finite(z[i]) && finite(w[i]))) off = 1;
+            kmax = fmaxf(kmax, fmaxf(__builtin_fabsf(x[i]), __builtin_fabsf(y[i]))), vmax = fmaxf(vmax, fmaxf(__builtin_fabsf(z[i]), __builtin_fabsf(w[i])));
+        }
+        auto most = [](float a, float b) { return fmaxf(a, b); };
+        const bool fine = over_lanes<LANES>(off, most) == 0;
+        char *kr = keys + r * ROW, *vr = values + r * ROW + 16 * j * ELEM;
+        if constexpr (ELEM == 2) {
+            *reinterpret_cast<uint4 *>(kr + 2 * u.c0) = kept(kh0, fine, 0x7e007e00u);
+            *reinterpret_cast<uint4 *>(kr + 2 * u.c1) = kept(kh1, fine, 0x7e007e00u);
+            *reinterpret_cast<uint4 *>(vr) = kept(v0, fine, 0);
+            *reinterpret_cast<uint4 *>(vr + 16) = kept(v1, fine, 0);
+        } else {
+            kmax = over_lanes<LANES>(kmax, most), vmax = over_lanes<LANES>(vmax, most);
+            const bool some_k = fine && kmax >= KV_NOTHING, some_v = fine && vmax >= KV_NOTHING;
+            const float inv_k = 127.0f / kmax, inv_v = 127.0f / vmax;
+            *reinterpret_cast<uint2 *>(kr + u.c0) = codes8(x, inv_k, some_k);
+            *reinterpret_cast<uint2 *>(kr + u.c1) = codes8(y, inv_k, some_k);
+            const uint2 c0 = codes8(z, inv_v, some_v), c1 = codes8(w, inv_v, some_v);
+            *reinterpret_cast<uint4 *>(vr) = make_uint4(c0.x, c0.y, c1.x, c1.y);
+            if (stored && j < 4) {
+                const int rest = s & (a.kv.page_size() - 1);
                 const float sk = !fine ? __builtin_nanf("") : some_k ? kmax / 127.0f : 0x1p-31f, sv = some_v ? vmax / 127.0f : 0x1p-31f;
                 const float out = j == 0 ? sk : j == 1 ? sv : j == 2 ? log2f(sv) : 1.0f / sv;
-                reinterpret_cast<float *>(block + kv_scale_offset(D))[j * KV_BLOCK + token] = out;
+                reinterpret_cast<float *>(a.kv.block(s >> a.kv.page_shift, head, rest) + kv_scale_offset(D))[j * KV_BLOCK + rest % KV_BLOCK] = out;
             }
         }
-        *reinterpret_cast<uint4 *>(mine) = make_uint4(c0.x, c0.y, c1.x, c1.y);
     }
+    if (tid < 64) find_pieces<ELEM, TILE>(p, a.slots, t0, a.T, a.kv);
     __syncthreads();
-    const int c = tid % D;                                // a channel per thread, every second piece
+#pragma unroll
+    for (int i = tid; i < TILE * D * ELEM / 16; i += 2 * D) {   // keys: 16 bytes, neighbouring lanes neighbouring tokens
+        const int row = i % TILE, piece = i / TILE, s = p.slot[row], in_page = s & (a.kv.page_size() - 1);
+        if (s < 0) continue;
+        *reinterpret_cast<uint4 *>(a.kv.block(s >> a.kv.page_shift, head, in_page) + kv_key_offset<ELEM>(in_page % KV_BLOCK, piece * 16 / ELEM)) =
+            *reinterpret_cast<const uint4 *>(keys + row * ROW + 16 * piece);
+    }
+    const int c = tid % D;                                // values: a channel per thread, every second piece
     for (int i = tid / D; i < p.count; i += 2) {
         const int row = p.row[i], kind = p.kind[i], s = p.slot[row], in_page = s & (a.kv.page_size() - 1);
         char *to = a.kv.block(s >> a.kv.page_shift, head, in_page) + kv_value_offset<ELEM>(in_page % KV_BLOCK, c, D);
@@ -364,7 +370,7 @@ __global__ __launch_bounds__(2 * D) void kv_append_kernel(AppendArgs a)
             };
             if (kind == WHOLE) *reinterpret_cast<uint4 *>(to) = make_uint4(two(0), two(2), two(8), two(10));
             else if (kind == FOUR) *reinterpret_cast<uint2 *>(to) = make_uint2(two(0), two(2));
-            else *reinterpret_cast<uint16_t *>(to) = (uint16_t)two(0);
+            else *reinterpret_cast<uint16_t *>(to) = *reinterpret_cast<const uint16_t *>(values + row * ROW + 2 * c);
         } else {
             auto four = [&](int k) {
                 const uint8_t *from = reinterpret_cast<const uint8_t *>(values) + (row + k) * ROW + c;
@@ -377,83 +383,103 @@ __global__ __launch_bounds__(2 * D) void kv_append_kernel(AppendArgs a)
     }
 }
 
-template <int ELEM, int D>
+template <int ELEM, int D, int TILE>
 __global__ __launch_bounds__(2 * D) void kv_read_kernel(KvView kv, const int32_t *__restrict__ slots, int T, __half *__restrict__ k, int64_t ldk,
                                                         __half *__restrict__ v, int64_t ldv)
 {
-    constexpr int LANES = D / 16, ROW = ELEM * D + 16;
-    __shared__ Pieces p;
-    __shared__ __attribute__((aligned(16))) char values[TILE * ROW];
+    constexpr int LANES = D / 16, ROW = ELEM * D + 16, KN = TILE * D * ELEM / 16 / (2 * D) > 0 ? TILE * D * ELEM / 16 / (2 * D) : 1;
+    __shared__ Pieces<TILE> p;
+    __shared__ __attribute__((aligned(16))) char keys[TILE * ROW], values[TILE * ROW];
     const int tid = threadIdx.x, head = blockIdx.x % kv.heads, t0 = blockIdx.x / kv.heads * TILE;
-    if (tid < 64) find_pieces<ELEM>(p, slots, t0, T, kv);
+    if (tid < 64) find_pieces<ELEM, TILE>(p, slots, t0, T, kv);
     __syncthreads();
+    uint4 kx[KN];
+    if (k) {
+#pragma unroll
+        for (int i = 0; i < KN; ++i) {                    // 16 bytes, neighbouring lanes neighbouring tokens
+            const int at = i * 2 * D + tid, row = at % TILE, piece = at / TILE, s = p.slot[row], in_page = s & (kv.page_size() - 1);
+            kx[i] = make_uint4(0, 0, 0, 0);
+            if (s >= 0 && piece < D * ELEM / 16)
+                kx[i] = *reinterpret_cast<const uint4 *>(kv.block(s >> kv.page_shift, head, in_page) + kv_key_offset<ELEM>(in_page % KV_BLOCK, piece * 16 / ELEM));
+        }
+    }
     const int c = tid % D;
     if (v) {
-        for (int i = tid / D; i < p.count; i += 2) {
-            const int row = p.row[i], kind = p.kind[i], s = p.slot[row], in_page = s & (kv.page_size() - 1);
-            const char *from = kv.block(s >> kv.page_shift, head, in_page) + kv_value_offset<ELEM>(in_page % KV_BLOCK, c, D);
-            if constexpr (ELEM == 2) {
-                auto put = [&](int k, unsigned w) {
-                    char *to = values + (row + k) * ROW + 2 * c;
-                    *reinterpret_cast<uint16_t *>(to) = (uint16_t)w, *reinterpret_cast<uint16_t *>(to + ROW) = (uint16_t)(w >> 16);
-                };
-                if (kind == WHOLE) {
-                    const uint4 w = *reinterpret_cast<const uint4 *>(from);
-                    put(0, w.x), put(2, w.y), put(8, w.z), put(10, w.w);
-                } else if (kind == FOUR) {
-                    const uint2 w = *reinterpret_cast<const uint2 *>(from);
-                    put(0, w.x), put(2, w.y);
+        const int count = p.count;
+        for (int i0 = tid / D; i0 < count; i0 += 8) {     // four pieces on their way at a time
+            uint4 got[4];
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                const int i = i0 + 2 * n;
+                if (i >= count) continue;
+                const int kind = p.kind[i], s = p.slot[p.row[i]], in_page = s & (kv.page_size() - 1);
+                const char *from = kv.block(s >> kv.page_shift, head, in_page) + kv_value_offset<ELEM>(in_page % KV_BLOCK, c, D);
+                if (kind == WHOLE) got[n] = *reinterpret_cast<const uint4 *>(from);
+                else if (kind == FOUR && ELEM == 2) got[n].x = *reinterpret_cast<const unsigned *>(from), got[n].y = *reinterpret_cast<const unsigned *>(from + 4);
+                else if (kind == FOUR) got[n].x = *reinterpret_cast<const unsigned *>(from);
+                else got[n].x = ELEM == 2 ? *reinterpret_cast<const uint16_t *>(from) : *reinterpret_cast<const uint8_t *>(from);
+            }
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                const int i = i0 + 2 * n;
+                if (i >= count) continue;
+                const int kind = p.kind[i];
+                char *to = values + p.row[i] * ROW + c * ELEM;
+                if constexpr (ELEM == 2) {
+                    auto put = [&](int k, unsigned w) { *reinterpret_cast<uint16_t *>(to + k * ROW) = (uint16_t)w, *reinterpret_cast<uint16_t *>(to + (k + 1) * ROW) = (uint16_t)(w >> 16); };
+                    if (kind == ONE) *reinterpret_cast<uint16_t *>(to) = (uint16_t)got[n].x;
+                    else put(0, got[n].x), put(2, got[n].y);
+                    if (kind == WHOLE) put(8, got[n].z), put(10, got[n].w);
                 } else {
-                    *reinterpret_cast<uint16_t *>(values + row * ROW + 2 * c) = *reinterpret_cast<const uint16_t *>(from);
-                }
-            } else {
-                auto put = [&](int k, unsigned w) {
-                    uint8_t *to = reinterpret_cast<uint8_t *>(values) + (row + k) * ROW + c;
-                    to[0] = (uint8_t)w, to[ROW] = (uint8_t)(w >> 8), to[2 * ROW] = (uint8_t)(w >> 16), to[3 * ROW] = (uint8_t)(w >> 24);
-                };
-                if (kind == WHOLE) {
-                    const uint4 w = *reinterpret_cast<const uint4 *>(from);
-                    put(0, w.x), put(8, w.y), put(16, w.z), put(24, w.w);
-                } else if (kind == FOUR) {
-                    put(0, *reinterpret_cast<const unsigned *>(from));
-                } else {
-                    *(reinterpret_cast<uint8_t *>(values) + row * ROW + c) = *reinterpret_cast<const uint8_t *>(from);
+                    auto put = [&](int k, unsigned w) {
+#pragma unroll
+                        for (int b = 0; b < 4; ++b) *reinterpret_cast<uint8_t *>(to + (k + b) * ROW) = (uint8_t)(w >> (8 * b));
+                    };
+                    if (kind == ONE) *reinterpret_cast<uint8_t *>(to) = (uint8_t)got[n].x;
+                    else put(0, got[n].x);
+                    if (kind == WHOLE) put(8, got[n].y), put(16, got[n].z), put(24, got[n].w);
                 }
             }
         }
-        __syncthreads();
     }
+    if (k) {
+#pragma unroll
+        for (int i = 0; i < KN; ++i) {
+            const int at = i * 2 * D + tid, row = at % TILE, piece = at / TILE;
+            if (piece < D * ELEM / 16) *reinterpret_cast<uint4 *>(keys + row * ROW + 16 * piece) = kx[i];
+        }
+    }
+    __syncthreads();
     const int r = tid / LANES, j = tid % LANES, t = t0 + r;
-    if (t >= T) return;
-    const int slot = p.slot[r], rest = slot & (kv.page_size() - 1), token = rest % KV_BLOCK;
-    const char *block = slot < 0 ? nullptr : kv.block(slot >> kv.page_shift, head, rest);
+    if (r >= TILE || t >= T) return;
+    const int slot = p.slot[r], rest = slot & (kv.page_size() - 1);
     float sk = 0, sv = 0;
     if (ELEM == 1 && slot >= 0) {
-        const float *s = reinterpret_cast<const float *>(block + kv_scale_offset(D));
-        sk = s[token], sv = s[KV_BLOCK + token];
+        const float *s = reinterpret_cast<const float *>(kv.block(slot >> kv.page_shift, head, rest) + kv_scale_offset(D)) + rest % KV_BLOCK;
+        sk = s[0], sv = s[KV_BLOCK];
     }
-    auto scaled = [&](uint2 w, float s) {
-        float f[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = (float)((int)((i < 4 ? w.x : w.y) >> (8 * (i % 4)) & 255u) - 128) * s;
-        return narrow8(f);
-    };
-    const uint4 none = make_uint4(0, 0, 0, 0);
-    auto store = [&](__half *to, int64_t ld, const char *piece, int second, float s) {   // 16 channels; fp16: in two runs of 8
-        uint4 a = none, b = none;
+    auto store = [&](__half *to, const char *from, float scale) {   // 16 channels
+        uint4 a = make_uint4(0, 0, 0, 0), b = a;
         if (slot >= 0) {
+            const uint4 w = *reinterpret_cast<const uint4 *>(from);
             if constexpr (ELEM == 2) {
-                a = *reinterpret_cast<const uint4 *>(piece), b = *reinterpret_cast<const uint4 *>(piece + second);
+                a = w, b = *reinterpret_cast<const uint4 *>(from + 16);
             } else {
-                const uint4 w = *reinterpret_cast<const uint4 *>(piece);
-                a = scaled(make_uint2(w.x, w.y), s), b = scaled(make_uint2(w.z, w.w), s);
+                const unsigned x[4] = {w.x, w.y, w.z, w.w};
+                float f[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) f[i] = (float)((int)(x[i / 4] >> (8 * (i % 4)) & 255u) - 128) * scale;
+                float lo[8], hi[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) lo[i] = f[i], hi[i] = f[8 + i];
+                a = narrow8(lo), b = narrow8(hi);
             }
         }
-        __half *dst = to + t * ld + (int64_t)head * D + 16 * j;
-        *reinterpret_cast<uint4 *>(dst) = a, *reinterpret_cast<uint4 *>(dst + 8) = b;
+        *reinterpret_cast<uint4 *>(to) = a, *reinterpret_cast<uint4 *>(to + 8) = b;
     };
-    if (k) store(k, ldk, slot < 0 ? nullptr : block + kv_key_offset<ELEM>(token, 16 * j), 512, sk);
-    if (v) store(v, ldv, values + r * ROW + 16 * j * ELEM, 16, sv);
+    const int64_t at = (int64_t)head * D + 16 * j;
+    if (k) store(k + t * ldk + at, keys + r * ROW + 16 * j * ELEM, sk);
+    if (v) store(v + t * ldv + at, values + r * ROW + 16 * j * ELEM, sv);
 }
 
 __global__ void kv_no_requests_kernel(const int32_t *pool, int32_t *pool_out, int32_t *cu_new)
@@ -493,14 +519,22 @@ int launch_kv_resize(const int32_t *old_len, const int32_t *want_len, int reques
         }                                                                         \
     } while (0)
 
+// Rows of a workgroup: few tokens are mostly single ones, whose pieces are moved one after the other, and fill few workgroups.
+static int tile_rows(int T) { return T <= 256 ? 8 : 32; }
+
 int launch_kv_append(const __half *q, int64_t ldq, const __half *k, int64_t ldk, const __half *v, int64_t ldv, int T, int q_heads,
                      const float *cos_sin, int rotary, int max_positions, const int32_t *positions, const int32_t *slots,
                      __half *q_out, int64_t ldqo, const KvView &kv, hipStream_t st)
 {
-    const int64_t pairs = (int64_t)T * q_heads, kv_groups = (int64_t)ceil_div(T, TILE) * kv.heads, grid = kv_groups + (pairs + TILE - 1) / TILE;
+    const int tile = tile_rows(T);
+    const int64_t pairs = (int64_t)T * q_heads, kv_groups = (int64_t)ceil_div(T, tile) * kv.heads, grid = kv_groups + (pairs + 31) / 32;
     if (grid >= (int64_t)1 << 31) return fail(QL_ERR_UNSUPPORTED, "%d tokens of %d and %d heads are more than a launch holds", T, q_heads, kv.heads);
     const AppendArgs a = {q, k, v, ldq, ldk, ldv, ldqo, q_out, cos_sin, positions, slots, T, q_heads, rotary, max_positions, (int)kv_groups, kv};
-#define QL_CALL(E, D) kv_append_kernel<E, D><<<(unsigned)grid, 2 * D, 0, st>>>(a)
+#define QL_CALL(E, D)                                                                 \
+    do {                                                                              \
+        if (tile == 8) kv_append_kernel<E, D, 8><<<(unsigned)grid, 2 * D, 0, st>>>(a); \
+        else kv_append_kernel<E, D, 32><<<(unsigned)grid, 2 * D, 0, st>>>(a);         \
+    } while (0)
     QL_KV_DISPATCH(kv, QL_CALL);
 #undef QL_CALL
     return check_hip(hipGetLastError(), "kv_append_kernel");
@@ -508,9 +542,14 @@ int launch_kv_append(const __half *q, int64_t ldq, const __half *k, int64_t ldk,
 
 int launch_kv_read(const KvView &kv, const int32_t *slots, int T, __half *k, int64_t ldk, __half *v, int64_t ldv, hipStream_t st)
 {
-    const int64_t grid = (int64_t)ceil_div(T, TILE) * kv.heads;
+    const int tile = tile_rows(T);
+    const int64_t grid = (int64_t)ceil_div(T, tile) * kv.heads;
     if (grid >= (int64_t)1 << 31) return fail(QL_ERR_UNSUPPORTED, "%d tokens of %d heads are more than a launch holds", T, kv.heads);
-#define QL_CALL(E, D) kv_read_kernel<E, D><<<(unsigned)grid, 2 * D, 0, st>>>(kv, slots, T, k, ldk, v, ldv)
+#define QL_CALL(E, D)                                                                                             \
+    do {                                                                                                          \
+        if (tile == 8) kv_read_kernel<E, D, 8><<<(unsigned)grid, 2 * D, 0, st>>>(kv, slots, T, k, ldk, v, ldv);   \
+        else kv_read_kernel<E, D, 32><<<(unsigned)grid, 2 * D, 0, st>>>(kv, slots, T, k, ldk, v, ldv);            \
+    } while (0)
     QL_KV_DISPATCH(kv, QL_CALL);
 #undef QL_CALL
     return check_hip(hipGetLastError(), "kv_read_kernel");
