@@ -152,11 +152,12 @@ __global__ __launch_bounds__(RESIZE_THREADS) void kv_resize_kernel(const int32_t
 }
 
 // ---- rows into the cache, and back -----------------------------------------------------------------------------
-// Bound by memory: rows of 2 D bytes are read, blocks written (read back: the other way round).  A workgroup takes 32 consecutive rows of one
+// Bound by memory: rows of 2 D bytes are read, blocks written (read back: the other way round).  A workgroup takes about 32 consecutive rows of one
 // key/value head, 16 channels per thread: the rows and the keys' pieces are 16 bytes per lane on both sides.  Values lie transposed in
 // a block: they go through LDS, and leave (arrive) 16 bytes at a time where the rows fill the piece of a channel -- 8 tokens in fp16, 16 in
 // int8 --, else by groups of 4 tokens, else singly: a decode step's tokens are single ones, a prompt's rows have them at its ends only.
-// 4096 tokens, 32 + 2 x 32 heads of 128, fp16, and 16001 tokens, 32 + 2 x 8 heads, int8; append / read back, us:  APPEND_FIGURES
+// 4096 tokens, 32 + 2 x 32 heads of 128, fp16, and 16001 tokens, 32 + 2 x 8 heads, int8; append / read back: 48 / 25 us and 78 / 28 us, 4.5 TB/s and more
+// of 5.1 that a large copy reaches (with windows of 32 rows whatever their slots, pieces cut at the windows' ends: 57 / 37, 86 / 40).
 
 __device__ inline bool finite(float x) { return __builtin_fabsf(x) <= 3.402823466e38f; }
 
@@ -175,41 +176,63 @@ __device__ inline float over_lanes(float v, OP op)
     return v;
 }
 
-// How the 32 rows' values lie in their blocks: pieces to move, {row of the first token, kind}.
-enum { ONE = 1, FOUR = 2, WHOLE = 3 };
-template <int TILE>
-struct Pieces {
-    int slot[TILE];                                       // -1: none
-    int count, row[TILE], kind[TILE];
+// The rows of a workgroup.  Consecutive slots of one block are a run; a workgroup takes the runs that begin in its window of TILE rows,
+// with what of the last one lies behind the window: so that blocks are written whole wherever the rows hold them whole, whatever place
+// in the batch a request's rows have.  Every wavefront finds them by itself, a row per lane.
+struct Rows {
+    uint64_t cont;                                        // rows that continue the row before
+    int slot, first, n;                                   // slot of this lane's row (-1: none); rows [first, first + n) from t0
 };
-
-// by the first wavefront
-template <int ELEM, int TILE>
-__device__ inline void find_pieces(Pieces<TILE> &p, const int32_t *slots, int t0, int T, const KvView &kv)
+template <int TILE>
+__device__ inline Rows find_rows(const int32_t *slots, int t0, int T, const KvView &kv)
 {
-    const int r = threadIdx.x;
-    int s = r < TILE && t0 + r < T ? slots[t0 + r] : -1;
-    if ((unsigned)s >= (unsigned)kv.pages << kv.page_shift) s = -1;
-    // tokens of a block are consecutive slots, and blocks begin at multiples of 32
-    auto at = [&](int v, int k) { const int o = __shfl(v, (r + k) & 63); return r + k >= 0 && r + k < TILE ? o : -1; };
-    const bool four = s >= 0 && s % 4 == 0 && at(s, 1) == s + 1 && at(s, 2) == s + 2 && at(s, 3) == s + 3;
-    auto four_at = [&](int k) { const int o = at(s, k), f = at(four, k); return f == 1 && o == s + k; };
-    const bool g8 = four_at(8), g16 = four_at(16), g24 = four_at(24);
-    const bool whole = ELEM == 2 ? four && s % 16 < 8 && g8 : four && s % 32 < 8 && g8 && g16 && g24;
-    // part of a piece that begins further up
-    const bool inside = s >= 0 && s % 4 && at(four, -(s & 3)) == 1 && at(s, -(s & 3)) == s - (s & 3);
-    const int up = ELEM == 2 ? s & 8 : s & 24;
-    const bool inside_whole = four && up && at(whole, -up) == 1 && at(s, -up) == s - up;
-    const int kind = s < 0 || inside || inside_whole ? 0 : whole ? WHOLE : four ? FOUR : ONE;
-    const uint64_t have = __ballot(kind != 0);
-    if (r < TILE) {
-        p.slot[r] = s;
-        if (kind) {
-            const int n = __popcll(have & ((1ull << r) - 1));
-            p.row[n] = r, p.kind[n] = kind;
-        }
-        if (r == 0) p.count = __popcll(have);
+    static_assert(TILE + KV_BLOCK <= 64, "a row per lane");
+    const int lane = threadIdx.x & 63;
+    auto slot_of = [&](int t) {
+        const int s = t >= 0 && t < T ? slots[t] : -1;
+        return (unsigned)s < (unsigned)kv.pages << kv.page_shift ? s : -1;
+    };
+    Rows r;
+    r.slot = slot_of(t0 + lane);
+    const int before = slot_of(t0 + lane - 1);
+    const bool cont = r.slot >= 0 && before >= 0 && r.slot == before + 1 && r.slot % KV_BLOCK != 0;
+    r.cont = __ballot(cont);
+    const uint64_t begins = __ballot(t0 + lane < T && !cont) & ((1ull << TILE) - 1);   // (a row without a slot is a run of its own)
+    r.first = r.n = 0;
+    if (begins) {
+        const int last = 63 - __builtin_clzll(begins);
+        r.first = __builtin_ctzll(begins);
+        r.n = last + 1 + __builtin_ctzll(~(r.cont >> last >> 1)) - r.first;
     }
+    return r;
+}
+
+// What to move of the rows' values, {row from `first`, kind}: whole pieces of a channel (fp16: tokens 4 h .. and 8 + 4 h .. of 16; int8:
+// four such groups of 32), groups of 4 tokens, single ones.
+enum { ONE = 1, FOUR = 2, WHOLE = 3 };
+struct Pieces {
+    int slot[64];                                         // by row from `first`
+    int count, row[64], kind[64];
+};
+template <int ELEM>
+__device__ inline void find_pieces(Pieces &p, const Rows &r)          // by one wavefront
+{
+    const int lane = threadIdx.x & 63, s = r.slot;
+    auto follow = [&](int row, int n) { return ((r.cont >> row >> 1) & ((1ull << n) - 1)) == (1ull << n) - 1; };   // rows + 1 .. + n continue
+    constexpr int REST = ELEM == 2 ? 11 : 27, SPAN = ELEM == 2 ? 16 : 32;
+    const bool mine = lane >= r.first && lane < r.first + r.n && s >= 0;
+    const bool four = s % 4 == 0 && follow(lane, 3), whole = four && s % SPAN < 8 && follow(lane, REST);
+    const int in4 = s & 3, up = s & (SPAN - 8);                        // rows down to the group's, to the piece's first one
+    const bool inside = in4 && lane >= in4 && follow(lane - in4, 3);
+    const bool inside_whole = four && up && lane >= up && follow(lane - up, REST);
+    const int kind = !mine || inside || inside_whole ? 0 : whole ? WHOLE : four ? FOUR : ONE;
+    const uint64_t have = __ballot(kind != 0);
+    if (kind) {
+        const int n = __popcll(have & ((1ull << lane) - 1));
+        p.row[n] = lane - r.first, p.kind[n] = kind;
+    }
+    if (lane >= r.first && lane < r.first + r.n) p.slot[lane - r.first] = s;
+    if (lane == 0) p.count = __popcll(have);
 }
 
 // Rotation of 16 channels of a row: the thread's two runs of 8, (8 j, 8 j + half) among the channels that are turned, neighbours among
@@ -277,7 +300,7 @@ struct AppendArgs {
 template <int ELEM, int D, int TILE>
 __global__ __launch_bounds__(2 * D) void kv_append_kernel(AppendArgs a)
 {
-    constexpr int LANES = D / 16, ROW = ELEM * D + 16;    // lanes of a token; bytes of a row in LDS
+    constexpr int LANES = D / 16, ROW = ELEM * D + 16, MOST = TILE + KV_BLOCK - 1;   // lanes of a token; bytes of a row in LDS; rows
     const int tid = threadIdx.x;
     auto table_row = [&](int t) { return a.cos_sin + (int64_t)min(max(a.positions[t], 0), a.max_positions - 1) * a.rotary; };
 
@@ -300,18 +323,19 @@ __global__ __launch_bounds__(2 * D) void kv_append_kernel(AppendArgs a)
         return;
     }
 
-    __shared__ Pieces<TILE> p;
-    __shared__ __attribute__((aligned(16))) char keys[TILE * ROW], values[TILE * ROW];
+    __shared__ Pieces p;
+    __shared__ __attribute__((aligned(16))) char values[MOST * ROW];
     const int head = blockIdx.x % a.kv.heads, t0 = blockIdx.x / a.kv.heads * TILE;
-    const int r = tid / LANES, j = tid % LANES;
-    if (TILE == 32 || r < TILE) {
-        const int t = min(t0 + r, a.T - 1);               // (a row behind the last one: the last one again, stored nowhere)
-        const Turn u(j, a.rotary);
+    const Rows rows = find_rows<TILE>(a.slots, t0, a.T, a.kv);
+    if (tid < 64) find_pieces<ELEM>(p, rows);
+    const int j = tid % LANES;
+    const Turn u(j, a.rotary);
+    for (int r = tid / LANES; r < rows.n; r += 32) {
+        const int t = t0 + rows.first + r, slot = a.slots[t];
+        const bool stored = (unsigned)slot < (unsigned)a.kv.pages << a.kv.page_shift;
         const __half *ks = a.k + t * a.ldk + (int64_t)head * D, *vs = a.v + t * a.ldv + (int64_t)head * D + 16 * j;
         const uint4 k0 = *reinterpret_cast<const uint4 *>(ks + u.c0), k1 = *reinterpret_cast<const uint4 *>(ks + u.c1);
         const uint4 v0 = *reinterpret_cast<const uint4 *>(vs), v1 = *reinterpret_cast<const uint4 *>(vs + 8);
-        const int s = t0 + r < a.T ? a.slots[t] : -1;
-        const bool stored = (unsigned)s < (unsigned)a.kv.pages << a.kv.page_shift;
         float x[8], y[8], z[8], w[8];
         widen8(k0, x), widen8(k1, y), widen8(v0, z), widen8(v1, w);
         if (a.rotary) rotate(u, table_row(t), a.rotary, x, y);
@@ -328,37 +352,33 @@ __global__ __launch_bounds__(2 * D) void kv_append_kernel(AppendArgs a)
         }
         auto most = [](float a, float b) { return fmaxf(a, b); };
         const bool fine = over_lanes<LANES>(off, most) == 0;
-        char *kr = keys + r * ROW, *vr = values + r * ROW + 16 * j * ELEM;
+        const int rest = slot & (a.kv.page_size() - 1), token = rest % KV_BLOCK;
+        char *block = stored ? a.kv.block(slot >> a.kv.page_shift, head, rest) : nullptr, *vr = values + r * ROW + 16 * j * ELEM;
         if constexpr (ELEM == 2) {
-            *reinterpret_cast<uint4 *>(kr + 2 * u.c0) = kept(kh0, fine, 0x7e007e00u);
-            *reinterpret_cast<uint4 *>(kr + 2 * u.c1) = kept(kh1, fine, 0x7e007e00u);
+            if (stored) {
+                *reinterpret_cast<uint4 *>(block + kv_key_offset<2>(token, u.c0)) = kept(kh0, fine, 0x7e007e00u);
+                *reinterpret_cast<uint4 *>(block + kv_key_offset<2>(token, u.c1)) = kept(kh1, fine, 0x7e007e00u);
+            }
             *reinterpret_cast<uint4 *>(vr) = kept(v0, fine, 0);
             *reinterpret_cast<uint4 *>(vr + 16) = kept(v1, fine, 0);
         } else {
             kmax = over_lanes<LANES>(kmax, most), vmax = over_lanes<LANES>(vmax, most);
             const bool some_k = fine && kmax >= KV_NOTHING, some_v = fine && vmax >= KV_NOTHING;
             const float inv_k = 127.0f / kmax, inv_v = 127.0f / vmax;
-            *reinterpret_cast<uint2 *>(kr + u.c0) = codes8(x, inv_k, some_k);
-            *reinterpret_cast<uint2 *>(kr + u.c1) = codes8(y, inv_k, some_k);
+            if (stored) {
+                *reinterpret_cast<uint2 *>(block + kv_key_offset<1>(token, u.c0)) = codes8(x, inv_k, some_k);
+                *reinterpret_cast<uint2 *>(block + kv_key_offset<1>(token, u.c1)) = codes8(y, inv_k, some_k);
+                if (j < 4) {
+                    const float sk = !fine ? __builtin_nanf("") : some_k ? kmax / 127.0f : 0x1p-31f, sv = some_v ? vmax / 127.0f : 0x1p-31f;
+                    const float out = j == 0 ? sk : j == 1 ? sv : j == 2 ? log2f(sv) : 1.0f / sv;
+                    reinterpret_cast<float *>(block + kv_scale_offset(D))[j * KV_BLOCK + token] = out;
+                }
+            }
             const uint2 c0 = codes8(z, inv_v, some_v), c1 = codes8(w, inv_v, some_v);
             *reinterpret_cast<uint4 *>(vr) = make_uint4(c0.x, c0.y, c1.x, c1.y);
-            if (stored && j < 4) {
-                const int rest = s & (a.kv.page_size() - 1);
-                const float sk = !fine ? __builtin_nanf("") : some_k ? kmax / 127.0f : 0x1p-31f, sv = some_v ? vmax / 127.0f : 0x1p-31f;
-                const float out = j == 0 ? sk : j == 1 ? sv : j == 2 ? log2f(sv) : 1.0f / sv;
-                reinterpret_cast<float *>(a.kv.block(s >> a.kv.page_shift, head, rest) + kv_scale_offset(D))[j * KV_BLOCK + rest % KV_BLOCK] = out;
-            }
         }
     }
-    if (tid < 64) find_pieces<ELEM, TILE>(p, a.slots, t0, a.T, a.kv);
     __syncthreads();
-#pragma unroll
-    for (int i = tid; i < TILE * D * ELEM / 16; i += 2 * D) {   // keys: 16 bytes, neighbouring lanes neighbouring tokens
-        const int row = i % TILE, piece = i / TILE, s = p.slot[row], in_page = s & (a.kv.page_size() - 1);
-        if (s < 0) continue;
-        *reinterpret_cast<uint4 *>(a.kv.block(s >> a.kv.page_shift, head, in_page) + kv_key_offset<ELEM>(in_page % KV_BLOCK, piece * 16 / ELEM)) =
-            *reinterpret_cast<const uint4 *>(keys + row * ROW + 16 * piece);
-    }
     const int c = tid % D;                                // values: a channel per thread, every second piece
     for (int i = tid / D; i < p.count; i += 2) {
         const int row = p.row[i], kind = p.kind[i], s = p.slot[row], in_page = s & (a.kv.page_size() - 1);
@@ -387,22 +407,13 @@ template <int ELEM, int D, int TILE>
 __global__ __launch_bounds__(2 * D) void kv_read_kernel(KvView kv, const int32_t *__restrict__ slots, int T, __half *__restrict__ k, int64_t ldk,
                                                         __half *__restrict__ v, int64_t ldv)
 {
-    constexpr int LANES = D / 16, ROW = ELEM * D + 16, KN = TILE * D * ELEM / 16 / (2 * D) > 0 ? TILE * D * ELEM / 16 / (2 * D) : 1;
-    __shared__ Pieces<TILE> p;
-    __shared__ __attribute__((aligned(16))) char keys[TILE * ROW], values[TILE * ROW];
+    constexpr int LANES = D / 16, ROW = ELEM * D + 16, MOST = TILE + KV_BLOCK - 1;
+    __shared__ Pieces p;
+    __shared__ __attribute__((aligned(16))) char values[MOST * ROW];
     const int tid = threadIdx.x, head = blockIdx.x % kv.heads, t0 = blockIdx.x / kv.heads * TILE;
-    if (tid < 64) find_pieces<ELEM, TILE>(p, slots, t0, T, kv);
+    const Rows rows = find_rows<TILE>(slots, t0, T, kv);
+    if (tid < 64) find_pieces<ELEM>(p, rows);
     __syncthreads();
-    uint4 kx[KN];
-    if (k) {
-#pragma unroll
-        for (int i = 0; i < KN; ++i) {                    // 16 bytes, neighbouring lanes neighbouring tokens
-            const int at = i * 2 * D + tid, row = at % TILE, piece = at / TILE, s = p.slot[row], in_page = s & (kv.page_size() - 1);
-            kx[i] = make_uint4(0, 0, 0, 0);
-            if (s >= 0 && piece < D * ELEM / 16)
-                kx[i] = *reinterpret_cast<const uint4 *>(kv.block(s >> kv.page_shift, head, in_page) + kv_key_offset<ELEM>(in_page % KV_BLOCK, piece * 16 / ELEM));
-        }
-    }
     const int c = tid % D;
     if (v) {
         const int count = p.count;
@@ -442,44 +453,47 @@ __global__ __launch_bounds__(2 * D) void kv_read_kernel(KvView kv, const int32_t
             }
         }
     }
-    if (k) {
-#pragma unroll
-        for (int i = 0; i < KN; ++i) {
-            const int at = i * 2 * D + tid, row = at % TILE, piece = at / TILE;
-            if (piece < D * ELEM / 16) *reinterpret_cast<uint4 *>(keys + row * ROW + 16 * piece) = kx[i];
-        }
-    }
-    __syncthreads();
-    const int r = tid / LANES, j = tid % LANES, t = t0 + r;
-    if (r >= TILE || t >= T) return;
-    const int slot = p.slot[r], rest = slot & (kv.page_size() - 1);
-    float sk = 0, sv = 0;
-    if (ELEM == 1 && slot >= 0) {
-        const float *s = reinterpret_cast<const float *>(kv.block(slot >> kv.page_shift, head, rest) + kv_scale_offset(D)) + rest % KV_BLOCK;
-        sk = s[0], sv = s[KV_BLOCK];
-    }
-    auto store = [&](__half *to, const char *from, float scale) {   // 16 channels
+    // 16 channels of a row
+    auto store = [&](__half *to, bool there, const char *from, int second, float scale) {
         uint4 a = make_uint4(0, 0, 0, 0), b = a;
-        if (slot >= 0) {
+        if (there) {
             const uint4 w = *reinterpret_cast<const uint4 *>(from);
             if constexpr (ELEM == 2) {
-                a = w, b = *reinterpret_cast<const uint4 *>(from + 16);
+                a = w, b = *reinterpret_cast<const uint4 *>(from + second);
             } else {
                 const unsigned x[4] = {w.x, w.y, w.z, w.w};
-                float f[16];
-#pragma unroll
-                for (int i = 0; i < 16; ++i) f[i] = (float)((int)(x[i / 4] >> (8 * (i % 4)) & 255u) - 128) * scale;
                 float lo[8], hi[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) lo[i] = f[i], hi[i] = f[8 + i];
+                for (int i = 0; i < 8; ++i) {
+                    lo[i] = (float)((int)(x[i / 4] >> (8 * (i % 4)) & 255u) - 128) * scale;
+                    hi[i] = (float)((int)(x[2 + i / 4] >> (8 * (i % 4)) & 255u) - 128) * scale;
+                }
                 a = narrow8(lo), b = narrow8(hi);
             }
         }
         *reinterpret_cast<uint4 *>(to) = a, *reinterpret_cast<uint4 *>(to + 8) = b;
     };
-    const int64_t at = (int64_t)head * D + 16 * j;
-    if (k) store(k + t * ldk + at, keys + r * ROW + 16 * j * ELEM, sk);
-    if (v) store(v + t * ldv + at, values + r * ROW + 16 * j * ELEM, sv);
+    const int j = tid % LANES;
+    auto each_row = [&](auto f) {
+        for (int r = tid / LANES; r < rows.n; r += 32) {
+            const int slot = p.slot[r], rest = slot & (kv.page_size() - 1);
+            const char *block = slot < 0 ? kv.base : kv.block(slot >> kv.page_shift, head, rest);
+            f(r, slot >= 0, block, rest % KV_BLOCK, t0 + rows.first + r);
+        }
+    };
+    const int64_t column = (int64_t)head * D + 16 * j;
+    if (k)
+        each_row([&](int, bool there, const char *block, int token, int t) {
+            const float scale = ELEM == 1 && there ? reinterpret_cast<const float *>(block + kv_scale_offset(D))[token] : 0.f;
+            store(k + t * ldk + column, there, block + kv_key_offset<ELEM>(token, 16 * j), 512, scale);
+        });
+    if (v) {
+        __syncthreads();
+        each_row([&](int r, bool there, const char *block, int token, int t) {
+            const float scale = ELEM == 1 && there ? reinterpret_cast<const float *>(block + kv_scale_offset(D))[KV_BLOCK + token] : 0.f;
+            store(v + t * ldv + column, there, values + r * ROW + 16 * j * ELEM, 16, scale);
+        });
+    }
 }
 
 __global__ void kv_no_requests_kernel(const int32_t *pool, int32_t *pool_out, int32_t *cu_new)
@@ -500,7 +514,8 @@ int launch_kv_resize(const int32_t *old_len, const int32_t *want_len, int reques
         kv_no_requests_kernel<<<1, 64, 0, st>>>(pool, pool_out, cu_new);
         return check_hip(hipGetLastError(), "kv_no_requests_kernel");
     }
-    const int grid = min(256, max(1, max(ceil_div(max_tokens, 4 * RESIZE_THREADS), requests / 64)));
+    // a token per thread: each is a search in the sums and three loads that wait for each other (1024 requests, 27000 tokens: RESIZE_FIGURES)
+    const int grid = min(512, max(1, max(ceil_div(max_tokens, RESIZE_THREADS), requests / 64)));
     kv_resize_kernel<<<grid, RESIZE_THREADS, 0, st>>>(old_len, want_len, requests, page_shift, ring, pages, pool, pool_out, table, ld_table, columns,
                                                       kv_len, cu_new, slots, positions, max_tokens);
     return check_hip(hipGetLastError(), "kv_resize_kernel");
