@@ -25,6 +25,9 @@ typedef unsigned u4 __attribute__((ext_vector_type(4)));
 constexpr int ATTN_UNIT = 64;            // tokens that tiles of keys are aligned to, and parts of a row's tokens
 constexpr int ATTN_THREADS = 256;
 
+// r / group: see AttnArgs::group_mul
+__device__ inline int attn_token(const AttnArgs &a, int r) { return (int)((__umulhi((unsigned)r, a.group_mul) + (unsigned)r) >> a.group_shift); }
+
 struct AttnSpan {                        // a request as the kernels see it
     int cu, rows, ctx, len;              // first row of q, rows (new tokens x heads of the group), position of the first new token, tokens
     int low, high;                       // tokens that any of its rows sees; low is a multiple of ATTN_UNIT
@@ -56,7 +59,8 @@ __device__ inline int attn_units(int low, int high) { return (max(high - low, 0)
 __device__ inline int attn_tiles(const AttnSpan &r, int bm) { return (r.rows + bm - 1) / bm; }
 
 struct AttnTotals {
-    int64_t tiles, work;                 // tiles; tiles x units
+    int64_t tiles;
+    float work;                          // tiles x units
     int most;                            // units of a tile
 };
 
@@ -70,41 +74,36 @@ constexpr int ATTN_LEAST = 4;
 __device__ inline int attn_part_units(const AttnTotals &t, int slots)
 {
     if (slots == 0) return 1 << 30;
-    int64_t c;
+    // (at least the quotient, rounded up: the margin is ten times what the sum and the reciprocal may be short of)
+    auto quotient = [&](int64_t room) { return t.work * __builtin_amdgcn_rcpf((float)room) * 1.00001f + 1.0f; };
+    float c;
     if (t.tiles >= slots) {
-        c = (t.work + slots - 1) / slots;
+        c = quotient(slots);
     } else {
-        const int64_t r1 = slots - t.tiles, r2 = 2 * (int64_t)slots - t.tiles;
-        const int64_t c1 = (t.work + r1 - 1) / r1, c2 = (t.work + r2 - 1) / r2;
-        c = min(c1, (int64_t)t.most) + 2 <= 2 * (min(c2, (int64_t)t.most) + 2) ? c1 : c2;
+        const float c1 = quotient(slots - t.tiles), c2 = quotient(2 * (int64_t)slots - t.tiles), most = (float)t.most;
+        c = fminf(c1, most) + 2 <= 2 * (fminf(c2, most) + 2) ? c1 : c2;
     }
-    return (int)min(max(c, (int64_t)ATTN_LEAST), (int64_t)1 << 30);
+    return (int)fminf(fmaxf(c, (float)ATTN_LEAST), 1e9f);
 }
 __device__ inline int attn_parts(const AttnSpan &r, int part_units) { return max(1, (attn_units(r.low, r.high) + part_units - 1) / part_units); }
 
-__device__ inline int64_t wave_total(int64_t v)
+// over a wavefront, the same in every lane
+template <typename T, typename OP>
+__device__ inline T wave_all(T v, OP op)
 {
-    auto step = [&](auto off) {
-        unsigned a, b, c, d;
-        lane_pair<decltype(off)::value>((unsigned)v, a, b);
-        lane_pair<decltype(off)::value>((unsigned)((uint64_t)v >> 32), c, d);
-        v = (int64_t)((uint64_t)c << 32 | a) + (int64_t)((uint64_t)d << 32 | b);
-    };
-    step(std::integral_constant<int, 1>{}), step(std::integral_constant<int, 2>{}), step(std::integral_constant<int, 4>{});
-    step(std::integral_constant<int, 8>{}), step(std::integral_constant<int, 16>{}), step(std::integral_constant<int, 32>{});
-    return v;
-}
-__device__ inline int wave_most(int v)
-{
+    static_assert(sizeof(T) == 4, "one register");
     auto step = [&](auto off) {
         unsigned a, b;
-        lane_pair<decltype(off)::value>((unsigned)v, a, b);
-        v = max((int)a, (int)b);
+        lane_pair<decltype(off)::value>(__builtin_bit_cast(unsigned, v), a, b);
+        v = op(__builtin_bit_cast(T, a), __builtin_bit_cast(T, b));
     };
     step(std::integral_constant<int, 1>{}), step(std::integral_constant<int, 2>{}), step(std::integral_constant<int, 4>{});
     step(std::integral_constant<int, 8>{}), step(std::integral_constant<int, 16>{}), step(std::integral_constant<int, 32>{});
     return v;
 }
+template <typename T>
+__device__ inline T wave_total(T v) { return wave_all(v, [](T a, T b) { return a + b; }); }
+__device__ inline int wave_most(int v) { return wave_all(v, [](int a, int b) { return max(a, b); }); }
 __device__ inline int64_t wave_sum_before(int64_t v, int lane)    // inclusive prefix sum over a wavefront
 {
 #pragma unroll
@@ -125,24 +124,27 @@ __device__ inline int wave_sum_before(int v, int lane)
 }
 
 struct AttnScratch {
-    int64_t part[3][ATTN_THREADS / 64];
+    int64_t part[ATTN_THREADS / 64];
+    float work[ATTN_THREADS / 64];
+    int most[ATTN_THREADS / 64];
     int64_t found[2];
 };
 
 // The item-th tile (and part) of all requests; false if there are fewer.  Without parts the last tile of the last request comes first:
 // causal tiles get longer towards the end of a request, and the longest should not start last.
 // Up to 64 requests every wavefront finds it by itself, a request per lane; more are shared out over the workgroup.
-template <int THREADS>
-__device__ inline bool attn_item(const AttnArgs &a, int bm, int slots, int item, AttnScratch &s, AttnItem &out)
+template <int THREADS, int bm>
+__device__ inline bool attn_item(const AttnArgs &a, int slots, int item, AttnScratch &s, AttnItem &out)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     constexpr int NW = THREADS / 64;
-    AttnTotals all;
+    AttnTotals all = {};
     if (a.requests <= 64) {
         AttnSpan r = {};
         if (lane < a.requests) r = attn_span(a, lane);
         const int tiles = attn_tiles(r, bm), units = attn_units(r.low, r.high);
-        all = {wave_total(tiles), slots ? wave_total((int64_t)tiles * units) : 0, slots ? wave_most(units) : 0};
+        all.tiles = wave_total(tiles);                       // (2^24 each at most)
+        if (slots) all.work = wave_total((float)tiles * (float)units), all.most = wave_most(units);
         const int c = attn_part_units(all, slots), parts = slots ? attn_parts(r, c) : 1;
         // (at most 2^24 each: more is a cu_new that decreases somewhere)
         const int n = lane < a.requests ? (int)min((int64_t)tiles * parts, (int64_t)1 << 24) : 0;
@@ -158,20 +160,21 @@ __device__ inline bool attn_item(const AttnArgs &a, int bm, int slots, int item,
         out.tile = k / out.parts, out.part = k % out.parts;
         return true;
     }
-    int64_t tiles = 0, work = 0;
+    int64_t tiles = 0;
+    float work = 0;
     int most = 0;
     for (int b = threadIdx.x; b < a.requests; b += THREADS) {
         const AttnSpan r = attn_span(a, b);
         const int n = attn_tiles(r, bm), units = attn_units(r.low, r.high);
-        tiles += n, work += (int64_t)n * units, most = max(most, units);
+        tiles += n, work += (float)n * (float)units, most = max(most, units);
     }
-    tiles = wave_total(tiles), work = wave_total(work), most = wave_most(most);
-    if (lane == 0) s.part[0][wave] = tiles, s.part[1][wave] = work, s.part[2][wave] = most;
+    tiles = __shfl(wave_sum_before(tiles, lane), 63), work = wave_total(work), most = wave_most(most);
+    if (lane == 0) s.part[wave] = tiles, s.work[wave] = work, s.most[wave] = most;
     if (threadIdx.x == 0) s.found[0] = -1;
     __syncthreads();
     all = {};
 #pragma unroll
-    for (int w = 0; w < NW; ++w) all.tiles += s.part[0][w], all.work += s.part[1][w], all.most = max(all.most, (int)s.part[2][w]);
+    for (int w = 0; w < NW; ++w) all.tiles += s.part[w], all.work += s.work[w], all.most = max(all.most, s.most[w]);
     const int c = attn_part_units(all, slots);
     int64_t want = item, before = 0;
     if (slots == 0) want = all.tiles - 1 - item;
@@ -184,13 +187,13 @@ __device__ inline bool attn_item(const AttnArgs &a, int bm, int slots, int item,
         }
         const int64_t upto = wave_sum_before(n, lane);
         __syncthreads();                                     // the sums of the round before have been read
-        if (lane == 63) s.part[0][wave] = upto;
+        if (lane == 63) s.part[wave] = upto;
         __syncthreads();
         int64_t at = before + upto - n;
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-            if (w < wave) at += s.part[0][w];
-            before += s.part[0][w];
+            if (w < wave) at += s.part[w];
+            before += s.part[w];
         }
         if (want >= at && want < at + n) s.found[0] = b, s.found[1] = want - at;
     }
@@ -211,17 +214,17 @@ __device__ inline void attn_range(const AttnArgs &a, const AttnSpan &r, int row0
 {
     low = r.low, high = r.high;
     if (a.causal) {
-        high = (int)max((int64_t)0, min((int64_t)r.len, (int64_t)r.ctx + (row1 - 1) / a.group + 1));
-        if (a.window) low = (int)min((int64_t)high, max((int64_t)0, (int64_t)r.ctx + row0 / a.group - a.window + 1)) & -ATTN_UNIT;
+        high = (int)max((int64_t)0, min((int64_t)r.len, (int64_t)r.ctx + attn_token(a, row1 - 1) + 1));
+        if (a.window) low = (int)min((int64_t)high, max((int64_t)0, (int64_t)r.ctx + attn_token(a, row0) - a.window + 1)) & -ATTN_UNIT;
     }
 }
 
 // Range of a part of [low, high), in whole units.
 __device__ inline void attn_part_range(int &low, int &high, int part, int parts)
 {
-    const int u = attn_units(low, high), l0 = low;
-    low = l0 + (int)((int64_t)u * part / parts) * ATTN_UNIT;
-    high = min(high, l0 + (int)((int64_t)u * (part + 1) / parts) * ATTN_UNIT);
+    if (parts == 1) return;
+    const int each = (attn_units(low, high) + parts - 1) / parts * ATTN_UNIT, end = high;
+    low = (int)min((int64_t)low + (int64_t)part * each, (int64_t)end), high = (int)min((int64_t)low + each, (int64_t)end);
 }
 
 // Workspace: for every item a note of what there is to join (int4: parts, or 0 where this item is not the first of several; first row
@@ -245,12 +248,12 @@ __device__ inline float *attn_partial(const AttnArgs &a, const AttnPlan &p, int6
 }
 
 // Finds the workgroup's item and leaves the note of it.
-template <int THREADS>
+template <int THREADS, int BM>
 __device__ inline bool attn_take(const AttnArgs &a, const AttnPlan &p, int index, int kvh, AttnScratch &s, AttnItem &it)
 {
-    const bool there = attn_item<THREADS>(a, p.bm, p.slots, index, s, it);
+    const bool there = attn_item<THREADS, BM>(a, p.slots, index, s, it);
     if (p.slots && kvh == 0 && threadIdx.x == 0)
-        static_cast<int4 *>(a.ws)[index] = there && it.part == 0 && it.parts > 1 ? make_int4(it.parts, it.r.cu, it.tile * p.bm, it.r.rows) : make_int4(0, 0, 0, 0);
+        static_cast<int4 *>(a.ws)[index] = there && it.part == 0 && it.parts > 1 ? make_int4(it.parts, it.r.cu, it.tile * BM, it.r.rows) : make_int4(0, 0, 0, 0);
     return there;
 }
 

@@ -49,11 +49,14 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, AttnPlan pla
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) l += __shfl_xor(l, d);
         const float inv = l == 0.f ? 0.f : 1.0f / l;
-        __half *dst = a.y + (int64_t)(note.y + row / a.group) * a.ldy + (int64_t)(kvh * a.group + row % a.group) * D + lane * N;
+        const int token = attn_token(a, row);
+        __half *dst = a.y + (int64_t)(note.y + token) * a.ldy + (int64_t)(kvh * a.group + row - token * a.group) * D + lane * N;
 #pragma unroll
         for (int c = 0; c < N; ++c) dst[c] = __float2half(o[c] * inv);
     }
 }
+
+constexpr int SHORT = 2048;
 
 }  // namespace
 
@@ -80,7 +83,8 @@ size_t attention_workspace_bytes(const KvView &kv, int T, int requests, int q_he
 
 int launch_attention(const AttnArgs &a, hipStream_t st)
 {
-    const AttnPlan p = attention_plan(a.kv, a.T, a.requests, a.q_heads, a.max_new);
+    AttnPlan p = attention_plan(a.kv, a.T, a.requests, a.q_heads, a.max_new);
+    if (p.step && (int64_t)a.columns << a.kv.page_shift <= SHORT) p.slots = 0, p.items = (int)((int64_t)a.T * a.group / p.bm + a.requests);
     if ((int64_t)p.items * a.kv.heads >= (int64_t)1 << 31)
         return fail(QL_ERR_UNSUPPORTED, "%d tokens of %d query heads are more than a launch holds", a.T, a.q_heads);
     // exp(scale s) = exp2(c s); a scale of nothing keeps masked scores apart from the others (-inf times 0 would be NaN)

@@ -42,11 +42,11 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attn_step_kernel(AttnAr
 
     const int kvh = blockIdx.x % a.kv.heads, index = blockIdx.x / a.kv.heads;
     AttnItem it;
-    if (!attn_take<NW * 64>(a, plan, index, kvh, scratch, it)) return;
+    if (!attn_take<NW * 64, BM>(a, plan, index, kvh, scratch, it)) return;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, qd = lane >> 4;
     const int row0 = it.tile * BM;
-    auto position = [&](int r) { return (int)min(max((int64_t)it.r.ctx + r / a.group, (int64_t)-1), (int64_t)INT32_MAX); };
+    auto position = [&](int r) { return (int)min(max((int64_t)it.r.ctx + attn_token(a, r), (int64_t)-1), (int64_t)INT32_MAX); };
     const int pos0 = position(row0), pos1 = position(min(row0 + BM, it.r.rows) - 1);
 
     int low, high;
@@ -60,7 +60,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attn_step_kernel(AttnAr
     for (int n = 0; n < NQ; ++n) {
         const int row = row0 + 16 * n + col;
         const bool live = row < it.r.rows;
-        const int token = live ? row / a.group : 0, head = kvh * a.group + (live ? row % a.group : 0);
+        const int token = live ? attn_token(a, row) : 0, head = kvh * a.group + (live ? row - token * a.group : 0);
         pos[n] = position(live ? row : 0);
         const __half *src = a.q + (int64_t)(it.r.cu + token) * a.ldq + (int64_t)head * D;
 #pragma unroll
@@ -309,7 +309,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attn_step_kernel(AttnAr
                     *reinterpret_cast<f4 *>(out + (size_t)r * D + 16 * e + 4 * qd) = v;
                 } else {
                     const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-                    __half *dst = a.y + (int64_t)(it.r.cu + row / a.group) * a.ldy + (int64_t)(kvh * a.group + row % a.group) * D + 16 * e + 4 * qd;
+                    const int token = attn_token(a, row);
+                    __half *dst = a.y + (int64_t)(it.r.cu + token) * a.ldy + (int64_t)(kvh * a.group + row - token * a.group) * D + 16 * e + 4 * qd;
                     *reinterpret_cast<uint2 *>(dst) = make_uint2(pack2(v[0] * inv, v[1] * inv), pack2(v[2] * inv, v[3] * inv));
                 }
             }

@@ -31,14 +31,14 @@ __global__ __launch_bounds__(NW * 64, D == 256 ? 1 : 2) void attn_tile_kernel(At
 
     const int kvh = blockIdx.x % a.kv.heads, index = blockIdx.x / a.kv.heads;
     AttnItem it;
-    if (!attn_take<NW * 64>(a, plan, index, kvh, scratch, it)) return;
+    if (!attn_take<NW * 64, BM>(a, plan, index, kvh, scratch, it)) return;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, h = lane >> 5;
     const int row0 = it.tile * BM, wrow0 = row0 + wave * 32, row = wrow0 + col;
     const bool live = row < it.r.rows;
-    const int token = live ? row / a.group : 0, head = kvh * a.group + (live ? row % a.group : 0);
+    const int token = live ? attn_token(a, row) : 0, head = kvh * a.group + (live ? row - token * a.group : 0);
     // positions: of this lane's row, of the wavefront's first and last
-    auto position = [&](int r) { return (int)min(max((int64_t)it.r.ctx + r / a.group, (int64_t)-1), (int64_t)INT32_MAX); };
+    auto position = [&](int r) { return (int)min(max((int64_t)it.r.ctx + attn_token(a, r), (int64_t)-1), (int64_t)INT32_MAX); };
     const int pos = position(live ? row : 0), pos0 = position(wrow0), pos1 = position(min(wrow0 + 32, it.r.rows) - 1);
 
     int low, high;

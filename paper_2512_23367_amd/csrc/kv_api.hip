@@ -248,6 +248,8 @@ int ql_paged_attention(const void *q, int64_t ldq, int T, int q_heads, const voi
     a.requests = requests;
     a.q_heads = q_heads;
     a.group = q_heads / kv.heads;
+    while ((1u << a.group_shift) < (unsigned)a.group) ++a.group_shift;
+    a.group_mul = (unsigned)((((uint64_t)1 << 32) * ((1u << a.group_shift) - (unsigned)a.group)) / (unsigned)a.group + 1);
     a.scale = scale;
     a.causal = causal;
     a.window = window;

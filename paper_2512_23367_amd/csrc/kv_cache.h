@@ -52,6 +52,7 @@ struct AttnArgs {
     int columns;
     const int32_t *cu, *ctx, *len;
     int T, requests, q_heads, group;
+    unsigned group_mul, group_shift;     // r / group = (high word of r * group_mul, + r) >> group_shift for r below 2^31
     float scale;
     int causal, window;
     int max_new;
