@@ -6,7 +6,7 @@
 //
 // Lengths are known on the device only (a captured step is replayed with others).  The host launches as many workgroups as the sizes
 // that it knows allow for, and each finds its work from the lengths: request b has tiles_b = ceil(new_b G / bm) tiles and
-// parts_b = ceil(units_b / C) parts of each (units of 64 tokens); see attn_part_units for C.  Without parts (slots 0): one per tile.
+// parts_b = ceil(units_b / c) parts of each (units of 64 tokens); see attn_part_units for c.  Without parts (slots 0): one per tile.
 #pragma once
 
 #include <type_traits>
@@ -64,28 +64,9 @@ struct AttnTotals {
     int most;                            // units of a tile
 };
 
-// Units of a part, from the totals and the number of workgroups of a key/value head that run at the same time (`slots`).  In k rounds
-// over the slots there is room for k slots - tiles cuts, so that parts of work / (k slots - tiles) units suffice; each part costs
-// about two units on top (finding its work, the queries, joining).  One round, or two if that is shorter; where the tiles alone fill
-// the slots, parts of what a slot has on average.  No more than max(2 slots, tiles + slots) parts in all.
-// Decode steps, 8 heads, int8, against parts of work / slots units (a few more of them than slots): four requests of 60000..131072
-// tokens 150 us, 181; 32 requests of 200..4096 tokens 33 us, 39.
+// Parts of a tile's units, of about c each (any number covers them: see attn_part_range).
 constexpr int ATTN_LEAST = 4;
-__device__ inline int attn_part_units(const AttnTotals &t, int slots)
-{
-    if (slots == 0) return 1 << 30;
-    // (at least the quotient, rounded up: the margin is ten times what the sum and the reciprocal may be short of)
-    auto quotient = [&](int64_t room) { return t.work * __builtin_amdgcn_rcpf((float)room) * 1.00001f + 1.0f; };
-    float c;
-    if (t.tiles >= slots) {
-        c = quotient(slots);
-    } else {
-        const float c1 = quotient(slots - t.tiles), c2 = quotient(2 * (int64_t)slots - t.tiles), most = (float)t.most;
-        c = fminf(c1, most) + 2 <= 2 * (fminf(c2, most) + 2) ? c1 : c2;
-    }
-    return (int)fminf(fmaxf(c, (float)ATTN_LEAST), 1e9f);
-}
-__device__ inline int attn_parts(const AttnSpan &r, int part_units) { return max(1, (attn_units(r.low, r.high) + part_units - 1) / part_units); }
+__device__ inline int attn_parts(int units, float c) { return max(1, (int)(units * __builtin_amdgcn_rcpf(c) + 0.9999f)); }
 
 // over a wavefront, the same in every lane
 template <typename T, typename OP>
@@ -104,6 +85,35 @@ __device__ inline T wave_all(T v, OP op)
 template <typename T>
 __device__ inline T wave_total(T v) { return wave_all(v, [](T a, T b) { return a + b; }); }
 __device__ inline int wave_most(int v) { return wave_all(v, [](int a, int b) { return max(a, b); }); }
+// Units of a part.  `slots`: workgroups of a key/value head that two for every CU come to.
+// A CU streams keys and values at about 36 GB/s with two workgroups or more, at 27 with one of 16 rows, at 16 with one of more rows;
+// 256 CUs together no more than 6.2 TB/s: in units of a CU's 36 GB/s the time is the larger of 1.5 work / 256 and of (workgroups per CU,
+// rounded up) x (units of a part).  So their number is kept just below one or two for every CU, in as long parts as that gives; where the
+// tiles alone are more, none is longer than the average.
+// Decode steps, 8 heads, int8, cut into work / slots units for 512 and for 256 workgroups (a few CUs get one more than the others): four
+// requests of 60000..131072 tokens 184, 193 us, this way 157; 32 requests of 200..4096 tokens 40, 37 us, this way 35; four new tokens
+// each (32 rows) on four requests of 30000..60000: one workgroup a CU 139 us, two 114.
+template <int bm, typename COUNT>
+__device__ inline float attn_part_units(float tiles, float work, float most, int slots, COUNT parts_of_all)
+{
+    const float half = (float)(slots / 2 > 0 ? slots / 2 : 1), least = (float)ATTN_LEAST;
+    auto average = [&](float n) { return fmaxf(work * __builtin_amdgcn_rcpf(n) * 1.00001f, least); };
+    float best = average((float)slots), best_time = INFINITY;
+    for (int r = 1; r <= 2; ++r) {
+        const float room = r * half;
+        if (tiles > room) continue;
+        float c = average(room), n = 0;
+        for (int i = 0; i < 6; ++i) {                                // (parts are whole ones: the average gives too many)
+            n = (float)parts_of_all(c);
+            if (n <= room) break;
+            c *= fmaxf(n * __builtin_amdgcn_rcpf(room), 1.04f);
+        }
+        const float time = fmaxf(1.5f * work, (r == 2 ? 2.0f : bm == 16 ? 1.33f : 2.25f) * fminf(c, most) * half) + 2 * r * half;
+        if (n <= room && time < best_time) best = c, best_time = time;
+    }
+    return best;
+}
+
 __device__ inline int64_t wave_sum_before(int64_t v, int lane)    // inclusive prefix sum over a wavefront
 {
 #pragma unroll
@@ -126,7 +136,6 @@ __device__ inline int wave_sum_before(int v, int lane)
 struct AttnScratch {
     int64_t part[ATTN_THREADS / 64];
     float work[ATTN_THREADS / 64];
-    int most[ATTN_THREADS / 64];
     int64_t found[2];
 };
 
@@ -138,17 +147,20 @@ __device__ inline bool attn_item(const AttnArgs &a, int slots, int item, AttnScr
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     constexpr int NW = THREADS / 64;
-    AttnTotals all = {};
     if (a.requests <= 64) {
         AttnSpan r = {};
         if (lane < a.requests) r = attn_span(a, lane);
         const int tiles = attn_tiles(r, bm), units = attn_units(r.low, r.high);
-        all.tiles = wave_total(tiles);                       // (2^24 each at most)
-        if (slots) all.work = wave_total((float)tiles * (float)units), all.most = wave_most(units);
-        const int c = attn_part_units(all, slots), parts = slots ? attn_parts(r, c) : 1;
+        const int all = wave_total(tiles);                   // (2^24 each at most)
+        int parts = 1;
+        if (slots) {
+            auto count = [&](float c) { return wave_total((float)tiles * (float)attn_parts(units, c)); };
+            const float c = attn_part_units<bm>((float)all, wave_total((float)tiles * (float)units), (float)wave_most(units), slots, count);
+            parts = attn_parts(units, c);
+        }
         // (at most 2^24 each: more is a cu_new that decreases somewhere)
         const int n = lane < a.requests ? (int)min((int64_t)tiles * parts, (int64_t)1 << 24) : 0;
-        if (slots == 0) item = (int)min(all.tiles, (int64_t)1 << 30) - 1 - item;
+        if (slots == 0) item = all - 1 - item;
         const int upto = wave_sum_before(n, lane);
         const uint64_t owner = __ballot(item >= 0 && item < upto);
         if (!owner) return false;
@@ -162,28 +174,27 @@ __device__ inline bool attn_item(const AttnArgs &a, int slots, int item, AttnScr
     }
     int64_t tiles = 0;
     float work = 0;
-    int most = 0;
     for (int b = threadIdx.x; b < a.requests; b += THREADS) {
         const AttnSpan r = attn_span(a, b);
-        const int n = attn_tiles(r, bm), units = attn_units(r.low, r.high);
-        tiles += n, work += (float)n * (float)units, most = max(most, units);
+        const int n = attn_tiles(r, bm);
+        tiles += n, work += (float)n * (float)attn_units(r.low, r.high);
     }
-    tiles = __shfl(wave_sum_before(tiles, lane), 63), work = wave_total(work), most = wave_most(most);
-    if (lane == 0) s.part[wave] = tiles, s.work[wave] = work, s.most[wave] = most;
+    tiles = __shfl(wave_sum_before(tiles, lane), 63), work = wave_total(work);
+    if (lane == 0) s.part[wave] = tiles, s.work[wave] = work;
     if (threadIdx.x == 0) s.found[0] = -1;
     __syncthreads();
-    all = {};
+    tiles = 0, work = 0;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) all.tiles += s.part[w], all.work += s.work[w], all.most = max(all.most, s.most[w]);
-    const int c = attn_part_units(all, slots);
+    for (int w = 0; w < NW; ++w) tiles += s.part[w], work += s.work[w];
+    const float c = slots ? fmaxf(work * __builtin_amdgcn_rcpf((float)slots) * 1.00001f, (float)ATTN_LEAST) : 0.f;
     int64_t want = item, before = 0;
-    if (slots == 0) want = all.tiles - 1 - item;
+    if (slots == 0) want = tiles - 1 - item;
     for (int base = 0; base < a.requests && before <= want; base += THREADS) {
         const int b = base + threadIdx.x;
         int64_t n = 0;
         if (b < a.requests) {
             const AttnSpan r = attn_span(a, b);
-            n = (int64_t)attn_tiles(r, bm) * (slots ? attn_parts(r, c) : 1);
+            n = (int64_t)attn_tiles(r, bm) * (slots ? attn_parts(attn_units(r.low, r.high), c) : 1);
         }
         const int64_t upto = wave_sum_before(n, lane);
         __syncthreads();                                     // the sums of the round before have been read
@@ -204,7 +215,7 @@ __device__ inline bool attn_item(const AttnArgs &a, int slots, int item, AttnScr
     const AttnSpan r = attn_span(a, out.b);
     auto same = [&](int v) { return __builtin_amdgcn_readfirstlane(v); };
     out.r = {same(r.cu), same(r.rows), same(r.ctx), same(r.len), same(r.low), same(r.high)};
-    out.parts = same(slots ? attn_parts(out.r, c) : 1);
+    out.parts = same(slots ? attn_parts(attn_units(r.low, r.high), c) : 1);
     out.tile = k / out.parts, out.part = k % out.parts;
     return true;
 }
@@ -236,7 +247,7 @@ __host__ __device__ inline size_t attn_notes_bytes(int items) { return ((size_t)
 struct AttnPlan {
     int bm;              // rows of a tile
     int step;            // 1: the kernel for few rows, whose wavefronts share a tile's tokens
-    int slots;           // workgroups of a key/value head that run at the same time (0: a workgroup per tile, no parts)
+    int slots;           // two workgroups for every CU, per key/value head (0: a workgroup per tile, no parts)
     int items;           // workgroups of a key/value head
     size_t ws_bytes;
 };

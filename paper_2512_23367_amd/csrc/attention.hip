@@ -1,4 +1,5 @@
 // Attention over the paged cache: which kernel takes a call, and the sum of partial results (include/qlinear.h).
+#include <algorithm>
 #include <cmath>
 
 #include "attention.h"
@@ -56,7 +57,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, AttnPlan pla
     }
 }
 
-constexpr int SHORT = 2048;
+constexpr int SHORT = 1024;
 
 }  // namespace
 
@@ -68,10 +69,8 @@ AttnPlan attention_plan(const KvView &kv, int T, int requests, int q_heads, int 
     p.step = rows <= (kv.D == 256 ? 16 : 32);
     p.bm = !p.step ? 128 : rows <= 16 ? 16 : 32;
     const int64_t tiles = (int64_t)T * group / p.bm + requests;
-    // workgroups that the registers of a kernel leave room for on a CU, times 256 CUs
-    const int resident = 256 * (kv.D == 256 ? 1 : p.bm == 16 && kv.bits == 16 ? 3 : 2);
-    p.slots = !p.step && tiles * kv.heads >= resident ? 0 : ceil_div(resident, kv.heads);
-    p.items = (int)(p.slots ? (2 * (int64_t)p.slots > tiles + p.slots ? 2 * (int64_t)p.slots : tiles + p.slots) : tiles);
+    p.slots = !p.step && tiles * kv.heads >= 512 ? 0 : std::max(1, 512 / kv.heads);
+    p.items = (int)(tiles + p.slots);                                // tiles cut into c = work / slots units, or fewer
     p.ws_bytes = p.slots ? attn_notes_bytes(p.items) + (size_t)p.items * kv.heads * attn_partial_floats(p.bm, kv.D) * 4 : 0;
     return p;
 }
