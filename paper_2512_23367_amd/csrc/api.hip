@@ -243,7 +243,7 @@ int static_scratch(void **out)
 #pragma GCC visibility push(default)
 extern "C" {
 
-int ql_version(void) { return 100; }
+int ql_version(void) { return 200; }
 
 const char *ql_last_error(void) { return g_err; }
 

@@ -61,28 +61,48 @@ constexpr int SHORT = 1024;
 
 }  // namespace
 
-AttnPlan attention_plan(const KvView &kv, int T, int requests, int q_heads, int max_new)
+// Rows of a tile for requests of at most `rows` rows.  Fewer than 128: the kernel for few rows.  D = 256 leaves it registers for 16.
+static int tile_rows(int D, int64_t rows) { return rows <= 16 ? 16 : rows <= 32 && D < 256 ? 32 : 128; }
+
+static AttnPlan plan_of(const KvView &kv, int64_t tiles, int bm)
 {
     AttnPlan p = {};
-    const int group = q_heads / kv.heads;
-    const int64_t rows = (int64_t)(max_new && max_new < T ? max_new : T) * group;   // most of a request
-    p.step = rows <= (kv.D == 256 ? 16 : 32);
-    p.bm = !p.step ? 128 : rows <= 16 ? 16 : 32;
-    const int64_t tiles = (int64_t)T * group / p.bm + requests;
-    p.slots = !p.step && tiles * kv.heads >= 512 ? 0 : std::max(1, 512 / kv.heads);
+    p.bm = bm, p.step = bm < 128;
+    // cut where the tiles alone would leave CUs idle; tiles of few rows, whose lengths a single long request may dominate, as far as
+    // the partial results stay small
+    p.slots = tiles * kv.heads >= (p.step ? 4096 : 512) ? 0 : std::max(1, 512 / kv.heads);
     p.items = (int)(tiles + p.slots);                                // tiles cut into c = work / slots units, or fewer
-    p.ws_bytes = p.slots ? attn_notes_bytes(p.items) + (size_t)p.items * kv.heads * attn_partial_floats(p.bm, kv.D) * 4 : 0;
+    p.ws_bytes = p.slots ? attn_notes_bytes(p.items) + (size_t)p.items * kv.heads * attn_partial_floats(bm, kv.D) * 4 : 0;
     return p;
 }
+static int64_t most_rows(int T, int group, int max_new) { return (int64_t)(max_new && max_new < T ? max_new : T) * group; }
 
+AttnPlan attention_plan(const KvView &kv, int T, int requests, int q_heads, int max_new)
+{
+    const int group = q_heads / kv.heads, bm = tile_rows(kv.D, most_rows(T, group, max_new));
+    return plan_of(kv, (int64_t)T * group / bm + requests, bm);
+}
+
+// The most that a call with these sizes or smaller ones asks for.
 size_t attention_workspace_bytes(const KvView &kv, int T, int requests, int q_heads, int max_new)
 {
-    return attention_plan(kv, T, requests, q_heads, max_new).ws_bytes;
+    const int group = q_heads / kv.heads, largest = tile_rows(kv.D, most_rows(T, group, max_new));
+    size_t most = 0;
+    for (int bm : {16, 32, 128}) {
+        if (bm > largest) break;
+        const int64_t limit = ((bm < 128 ? 4096 : 512) - 1) / kv.heads;      // tiles of the largest call that is cut
+        most = std::max(most, plan_of(kv, std::min((int64_t)T * group / bm + requests, limit), bm).ws_bytes);
+    }
+    return most;
 }
 
 int launch_attention(const AttnArgs &a, hipStream_t st)
 {
     AttnPlan p = attention_plan(a.kv, a.T, a.requests, a.q_heads, a.max_new);
+    if (p.ws_bytes) {
+        if (!a.ws) return fail(QL_ERR_NULL, "ws is NULL");
+        if (a.ws_bytes < p.ws_bytes) return fail(QL_ERR_WORKSPACE, "workspace has %zu bytes, this call needs %zu (see ql_paged_attention_bytes)", a.ws_bytes, p.ws_bytes);
+    }
     if (p.step && (int64_t)a.columns << a.kv.page_shift <= SHORT) p.slots = 0, p.items = (int)((int64_t)a.T * a.group / p.bm + a.requests);
     if ((int64_t)p.items * a.kv.heads >= (int64_t)1 << 31)
         return fail(QL_ERR_UNSUPPORTED, "%d tokens of %d query heads are more than a launch holds", a.T, a.q_heads);

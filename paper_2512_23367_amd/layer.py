@@ -8,6 +8,14 @@ This is the prefill workload whose latency and weight memory the paper tabulates
 Evaluation, Table 3: INT8 against FP16); attention itself, the normalisations and the residual adds are not part of
 the quantized-linear path and are left out (the slice of the QKV output only makes the four GEMMs depend on each
 other the way a layer's do).
+
+    PagedDecoderLayer puts attention there: rotary embedding, the paged key/value cache and attention of the step's new
+    tokens over it.  PagedRequests keeps the books of the requests that share the cache's pages; it serves all layers of a
+    model, each of which has a cache of its own:
+
+        requests = PagedRequests(fmt, max_requests, columns, max_tokens)
+        requests.step(want_len)                                    # tokens per request after this step, int32 on the device
+        for layer, cache in zip(layers, caches): x = layer.forward(x, requests, cache)
 """
 from __future__ import annotations
 
@@ -23,7 +31,7 @@ class DecoderLayerLinears:
         self.bits, self.group = bits, (0 if bits == 8 else 128)
         self.d = w_o.shape[0]
         self.F = w_down.shape[1]
-        assert w_qkv.shape == (3 * self.d, self.d) and w_gate_up.shape == (2 * self.F, self.d) and w_down.shape == (self.d, self.F)
+        assert w_qkv.shape == self._qkv_shape(w_o) and w_gate_up.shape == (2 * self.F, self.d) and w_down.shape == (self.d, self.F)
         dev = w_o.device
         self.w = {}
         self.weight_bytes = 0
@@ -37,7 +45,7 @@ class DecoderLayerLinears:
             self.weight_bytes += kb + (sb if bits == 8 else 0)
         M = max_tokens
         self.max_tokens = M
-        self.y_qkv = torch.empty((M, 3 * self.d), dtype=torch.float16, device=dev)
+        self.y_qkv = torch.empty((M, w_qkv.shape[0]), dtype=torch.float16, device=dev)
         self.y_o = torch.empty((M, self.d), dtype=torch.float16, device=dev)
         self.y_gu = torch.empty((M, 2 * self.F), dtype=torch.float16, device=dev)
         self.y = torch.empty((M, self.d), dtype=torch.float16, device=dev)
@@ -45,6 +53,9 @@ class DecoderLayerLinears:
         self.sx = torch.empty(M, dtype=torch.float32, device=dev)
         ws = max(ql.ql_workspace_bytes(M, N, K, bits) for (_, _, _, N, K) in self.w.values())
         self.ws = torch.empty(ws, dtype=torch.uint8, device=dev)
+
+    def _qkv_shape(self, w_o):
+        return (3 * self.d, self.d)
 
     def _linear(self, x, name, y):
         kern, sw, bias, N, _ = self.w[name]
@@ -58,9 +69,14 @@ class DecoderLayerLinears:
         internal buffer, overwritten by the next call).  Everything is enqueued on torch's current stream."""
         M = x.shape[0]
         assert M <= self.max_tokens and x.shape[1] == self.d
-        y_qkv, y_o, y_gu, y = self.y_qkv[:M], self.y_o[:M], self.y_gu[:M], self.y[:M]
+        y_qkv = self.y_qkv[:M]
         self._linear(x, "qkv", y_qkv)
-        self._linear(y_qkv[:, :self.d], "o", y_o)
+        return self._behind_attention(y_qkv[:, :self.d])
+
+    def _behind_attention(self, y_attention):
+        M = y_attention.shape[0]
+        y_o, y_gu, y = self.y_o[:M], self.y_gu[:M], self.y[:M]
+        self._linear(y_attention, "o", y_o)
         self._linear(y_o, "gate_up", y_gu)
         ql.ql_quant_act_swiglu(y_gu, None, self.xq, self.sx)
         kern, sw, bias, N, K = self.w["down"]
@@ -69,3 +85,63 @@ class DecoderLayerLinears:
         else:
             ql.ql_w4a8_gemm(self.xq, self.sx, M, K, kern, self.group, bias, N, y, self.ws)
         return y
+
+
+class PagedRequests:
+    """The requests that share a cache's pages: block table, ring of free pages, and for the step at hand the slots and
+    positions of the new tokens.  All on the device; step() only enqueues, so a step can be captured into a HIP graph."""
+
+    def __init__(self, fmt: ql.QlKvFormat, max_requests: int, columns: int, max_tokens: int, device="cuda"):
+        """columns: pages that one request can have; max_tokens: new tokens of one step."""
+        ints = lambda *s: torch.zeros(s, dtype=torch.int32, device=device)  # noqa: E731
+        self.fmt, self.max_requests, self.max_tokens = fmt, max_requests, max_tokens
+        self.block_table = ints(max_requests, columns)
+        self.ring = torch.arange(fmt.pages, dtype=torch.int32, device=device)
+        self.pool = torch.tensor([0, fmt.pages, 0, 0], dtype=torch.int32, device=device)   # [2]: tokens that found no page
+        self.ctx_len, self.kv_len, self.cu_new = ints(max_requests), ints(max_requests), ints(max_requests + 1)
+        self.slots, self.positions = ints(max_tokens), ints(max_tokens)
+        self.max_new = 0
+
+    def step(self, want_len, max_new: int = 0):
+        """want_len int32 [max_requests]: tokens of every request after this step (0: none, its pages are free again; the
+        new tokens are the rows of the step's x, request after request).  max_new: the most new tokens of one request, if
+        known.  Rows behind the last new token (a padded batch) are computed, but neither stored nor attended to."""
+        self.max_new = max_new
+        self.ctx_len.copy_(self.kv_len)
+        self.slots.fill_(-1)
+        ql.ql_kv_resize(self.fmt.page_size, self.ctx_len, want_len, self.ring, self.pool, self.pool, self.block_table, self.kv_len,
+                        self.cu_new, self.slots, self.positions)
+
+
+class PagedDecoderLayer(DecoderLayerLinears):
+    """The four linears with attention over a paged cache between the QKV and the O projection."""
+
+    def __init__(self, w_qkv, w_o, w_gate_up, w_down, bits: int, max_tokens: int, fmt: ql.QlKvFormat, cos_sin, max_requests: int,
+                 biases=None, scale=None):
+        """w_qkv fp16 [(q_heads + 2 heads) head_dim, d], w_o [d, q_heads head_dim], the others as in DecoderLayerLinears; cos_sin:
+        rotary table of ql_kv_append; scale: of the scores, head_dim ** -0.5 by default."""
+        self.fmt, self.cos_sin = fmt, cos_sin
+        self.q_heads = w_o.shape[1] // fmt.head_dim
+        self.scale = fmt.head_dim ** -0.5 if scale is None else scale
+        super().__init__(w_qkv, w_o, w_gate_up, w_down, bits, max_tokens, biases)
+        self.y_attention = torch.zeros((max_tokens, self.q_heads * fmt.head_dim), dtype=torch.float16, device=w_o.device)
+        self.attention_ws = torch.empty(ql.ql_paged_attention_bytes(fmt, max_tokens, max_requests, self.q_heads), dtype=torch.uint8, device=w_o.device)
+        self.max_requests = max_requests
+
+    def _qkv_shape(self, w_o):
+        assert w_o.shape[1] == self.q_heads * self.fmt.head_dim
+        return ((self.q_heads + 2 * self.fmt.heads) * self.fmt.head_dim, self.d)
+
+    def forward(self, x, requests: PagedRequests, cache):
+        """x fp16 [M,d]: the new tokens of requests.step(), in its order; cache: this layer's, ql_kv_cache_bytes(fmt) bytes.
+        Returns fp16 [M,d], a view of an internal buffer that the next call overwrites."""
+        M, D = x.shape[0], self.fmt.head_dim
+        assert M <= min(self.max_tokens, requests.max_tokens) and requests.max_requests <= self.max_requests and x.shape[1] == self.d
+        y_qkv, y_attention = self.y_qkv[:M], self.y_attention[:M]
+        self._linear(x, "qkv", y_qkv)
+        nq, nk = self.q_heads * D, self.fmt.heads * D
+        q, k, v = y_qkv[:, :nq], y_qkv[:, nq:nq + nk], y_qkv[:, nq + nk:]
+        ql.ql_kv_append(q, k, v, self.cos_sin, requests.positions[:M], requests.slots[:M], q, cache, self.fmt)
+        ql.ql_paged_attention(q, cache, self.fmt, requests.block_table, requests.cu_new, requests.ctx_len, requests.kv_len, self.scale, y_attention,
+                              self.attention_ws, max_new=requests.max_new)
+        return self._behind_attention(y_attention)
