@@ -23,7 +23,7 @@ typedef float f16v __attribute__((ext_vector_type(16)));
 typedef unsigned u4 __attribute__((ext_vector_type(4)));
 
 constexpr int ATTN_UNIT = 64;            // tokens that tiles of keys are aligned to, and parts of a row's tokens
-constexpr int ATTN_THREADS = 256;
+constexpr int ATTN_THREADS = 512;
 
 // r / group: see AttnArgs::group_mul
 __device__ inline int attn_token(const AttnArgs &a, int r) { return (int)((__umulhi((unsigned)r, a.group_mul) + (unsigned)r) >> a.group_shift); }
@@ -36,6 +36,7 @@ struct AttnSpan {                        // a request as the kernels see it
 struct AttnItem {
     AttnSpan r;
     int b, tile, part, parts;
+    int item;                            // its number: parts of a tile follow each other
 };
 
 __device__ inline AttnSpan attn_span(const AttnArgs &a, int b)
@@ -58,12 +59,6 @@ __device__ inline int attn_units(int low, int high) { return (max(high - low, 0)
 
 __device__ inline int attn_tiles(const AttnSpan &r, int bm) { return (r.rows + bm - 1) / bm; }
 
-struct AttnTotals {
-    int64_t tiles;
-    float work;                          // tiles x units
-    int most;                            // units of a tile
-};
-
 // Parts of a tile's units, of about c each (any number covers them: see attn_part_range).
 constexpr int ATTN_LEAST = 4;
 __device__ inline int attn_parts(int units, float c) { return max(1, (int)(units * __builtin_amdgcn_rcpf(c) + 0.9999f)); }
@@ -85,18 +80,19 @@ __device__ inline T wave_all(T v, OP op)
 template <typename T>
 __device__ inline T wave_total(T v) { return wave_all(v, [](T a, T b) { return a + b; }); }
 __device__ inline int wave_most(int v) { return wave_all(v, [](int a, int b) { return max(a, b); }); }
+
 // Units of a part.  `slots`: workgroups of a key/value head that two for every CU come to.
-// A CU streams keys and values at about 36 GB/s with two workgroups or more, at 27 with one of 16 rows, at 16 with one of more rows;
-// 256 CUs together no more than 6.2 TB/s: in units of a CU's 36 GB/s the time is the larger of 1.5 work / 256 and of (workgroups per CU,
-// rounded up) x (units of a part).  So their number is kept just below one or two for every CU, in as long parts as that gives; where the
-// tiles alone are more, none is longer than the average.
+// A CU streams keys and values at about 36 GB/s with two workgroups or more, at 27 with one of 16 rows, at 16 with one of more
+// rows; 256 CUs together no more than 6.2 TB/s: in units of a CU's 36 GB/s the time is the larger of 1.5 work / 256 and of (workgroups per
+// CU, rounded up) x (units of a part).  So their number is kept just below one or two for every CU, in as long parts as that gives; where
+// the tiles alone are more, none is longer than the average.
 // Decode steps, 8 heads, int8, cut into work / slots units for 512 and for 256 workgroups (a few CUs get one more than the others): four
 // requests of 60000..131072 tokens 184, 193 us, this way 157; 32 requests of 200..4096 tokens 40, 37 us, this way 35; four new tokens
 // each (32 rows) on four requests of 30000..60000: one workgroup a CU 139 us, two 114.
 template <int bm, typename COUNT>
 __device__ inline float attn_part_units(float tiles, float work, float most, int slots, COUNT parts_of_all)
 {
-    const float half = (float)(slots / 2 > 0 ? slots / 2 : 1), least = (float)ATTN_LEAST;
+    const float least = (float)ATTN_LEAST, half = (float)max(slots / 2, 1);
     auto average = [&](float n) { return fmaxf(work * __builtin_amdgcn_rcpf(n) * 1.00001f, least); };
     float best = average((float)slots), best_time = INFINITY;
     for (int r = 1; r <= 2; ++r) {
@@ -108,7 +104,8 @@ __device__ inline float attn_part_units(float tiles, float work, float most, int
             if (n <= room) break;
             c *= fmaxf(n * __builtin_amdgcn_rcpf(room), 1.04f);
         }
-        const float time = fmaxf(1.5f * work, (r == 2 ? 2.0f : bm == 16 ? 1.33f : 2.25f) * fminf(c, most) * half) + 2 * r * half;
+        const float per = fminf(c, most);
+        const float time = fmaxf(1.5f * work, (r == 2 ? 2.0f : bm == 16 ? 1.33f : 2.25f) * per * half) + 2 * r * half;
         if (n <= room && time < best_time) best = c, best_time = time;
     }
     return best;
@@ -139,8 +136,8 @@ struct AttnScratch {
     int64_t found[2];
 };
 
-// The item-th tile (and part) of all requests; false if there are fewer.  Without parts the last tile of the last request comes first:
-// causal tiles get longer towards the end of a request, and the longest should not start last.
+// The workgroup's tile (and part): the last of all requests first, as causal tiles get longer towards the end of a request and the longest
+// should not start last (with more than 64 requests and parts, the first first); false if there are fewer.
 // Up to 64 requests every wavefront finds it by itself, a request per lane; more are shared out over the workgroup.
 template <int THREADS, int bm>
 __device__ inline bool attn_item(const AttnArgs &a, int slots, int item, AttnScratch &s, AttnItem &out)
@@ -151,17 +148,17 @@ __device__ inline bool attn_item(const AttnArgs &a, int slots, int item, AttnScr
         AttnSpan r = {};
         if (lane < a.requests) r = attn_span(a, lane);
         const int tiles = attn_tiles(r, bm), units = attn_units(r.low, r.high);
-        const int all = wave_total(tiles);                   // (2^24 each at most)
         int parts = 1;
         if (slots) {
+            const int all = wave_total(tiles);               // (2^24 each at most)
             auto count = [&](float c) { return wave_total((float)tiles * (float)attn_parts(units, c)); };
             const float c = attn_part_units<bm>((float)all, wave_total((float)tiles * (float)units), (float)wave_most(units), slots, count);
             parts = attn_parts(units, c);
         }
         // (at most 2^24 each: more is a cu_new that decreases somewhere)
         const int n = lane < a.requests ? (int)min((int64_t)tiles * parts, (int64_t)1 << 24) : 0;
-        if (slots == 0) item = all - 1 - item;
         const int upto = wave_sum_before(n, lane);
+        item = __builtin_amdgcn_readlane(upto, 63) - 1 - item;
         const uint64_t owner = __ballot(item >= 0 && item < upto);
         if (!owner) return false;
         out.b = __builtin_ctzll(owner);
@@ -169,7 +166,7 @@ __device__ inline bool attn_item(const AttnArgs &a, int slots, int item, AttnScr
         out.r = {of(r.cu), of(r.rows), of(r.ctx), of(r.len), of(r.low), of(r.high)};
         out.parts = of(parts);
         const int k = item - (of(upto) - of(n));
-        out.tile = k / out.parts, out.part = k % out.parts;
+        out.tile = k / out.parts, out.part = k % out.parts, out.item = item;
         return true;
     }
     int64_t tiles = 0;
@@ -186,7 +183,7 @@ __device__ inline bool attn_item(const AttnArgs &a, int slots, int item, AttnScr
     tiles = 0, work = 0;
 #pragma unroll
     for (int w = 0; w < NW; ++w) tiles += s.part[w], work += s.work[w];
-    const float c = slots ? fmaxf(work * __builtin_amdgcn_rcpf((float)slots) * 1.00001f, (float)ATTN_LEAST) : 0.f;
+    const float c = slots ? fmaxf(work * __builtin_amdgcn_rcpf((float)slots) * 1.00001f, (float)ATTN_LEAST) : 0.f;   // the average
     int64_t want = item, before = 0;
     if (slots == 0) want = tiles - 1 - item;
     for (int base = 0; base < a.requests && before <= want; base += THREADS) {
@@ -216,7 +213,7 @@ __device__ inline bool attn_item(const AttnArgs &a, int slots, int item, AttnScr
     auto same = [&](int v) { return __builtin_amdgcn_readfirstlane(v); };
     out.r = {same(r.cu), same(r.rows), same(r.ctx), same(r.len), same(r.low), same(r.high)};
     out.parts = same(slots ? attn_parts(attn_units(r.low, r.high), c) : 1);
-    out.tile = k / out.parts, out.part = k % out.parts;
+    out.tile = k / out.parts, out.part = k % out.parts, out.item = (int)want;
     return true;
 }
 
@@ -247,7 +244,7 @@ __host__ __device__ inline size_t attn_notes_bytes(int items) { return ((size_t)
 struct AttnPlan {
     int bm;              // rows of a tile
     int step;            // 1: the kernel for few rows, whose wavefronts share a tile's tokens
-    int slots;           // two workgroups for every CU, per key/value head (0: a workgroup per tile, no parts)
+    int slots;           // see attn_part_units (0: a workgroup per tile, no parts)
     int items;           // workgroups of a key/value head
     size_t ws_bytes;
 };
@@ -264,7 +261,7 @@ __device__ inline bool attn_take(const AttnArgs &a, const AttnPlan &p, int index
 {
     const bool there = attn_item<THREADS, BM>(a, p.slots, index, s, it);
     if (p.slots && kvh == 0 && threadIdx.x == 0)
-        static_cast<int4 *>(a.ws)[index] = there && it.part == 0 && it.parts > 1 ? make_int4(it.parts, it.r.cu, it.tile * BM, it.r.rows) : make_int4(0, 0, 0, 0);
+        static_cast<int4 *>(a.ws)[there ? it.item : index] = there && it.part == 0 && it.parts > 1 ? make_int4(it.parts, it.r.cu, it.tile * BM, it.r.rows) : make_int4(0, 0, 0, 0);
     return there;
 }
 

@@ -62,35 +62,47 @@ constexpr int SHORT = 1024;
 }  // namespace
 
 // Rows of a tile for requests of at most `rows` rows.  Fewer than 128: the kernel for few rows.  D = 256 leaves it registers for 16.
-static int tile_rows(int D, int64_t rows) { return rows <= 16 ? 16 : rows <= 32 && D < 256 ? 32 : 128; }
+// 256 rows: keys and values come to a CU once for all eight of its wavefronts instead of once for every four, whose every load costs
+// the instruction issue of ten vector operations; where there are such tiles for three CUs in four.
+// us, 128 / 256 rows, 32 + 8 heads: 16384 tokens fp16 2190 / 2080; 2 x 2048 on 9000 627 / 680; 4096, 32 + 32 heads, 171 / 151, int8 191 / 165;
+// 2048, 12 + 12 heads (108 tiles of 256) 52 / 52; D = 64, 8192 tokens int8 398 / 430.
+static int tile_rows(const KvView &kv, int T, int group, int max_new)
+{
+    const int64_t rows = (int64_t)(max_new && max_new < T ? max_new : T) * group;
+    if (rows <= 16) return 16;
+    if (rows <= 32 && kv.D < 256) return 32;
+    return kv.D == 128 && rows >= 256 && (int64_t)T * group / 256 * kv.heads >= 192 ? 256 : 128;
+}
+
+// Tiles of a call that is cut into parts, at most: where they are more, there is enough of them for every CU; tiles of few rows, whose
+// time a single long request may be, as far as the partial results stay small.  (Tiles of 256 rows cut into one to four parts for every
+// CU, against whole ones: 2 x 1000 tokens on 9000 and 17000 654 us, 647; 4096 tokens, 32 + 32 heads, 164, 155.)
+static int64_t most_tiles(int bm) { return bm == 256 ? 0 : bm == 128 ? 511 : 4095; }
 
 static AttnPlan plan_of(const KvView &kv, int64_t tiles, int bm)
 {
     AttnPlan p = {};
     p.bm = bm, p.step = bm < 128;
-    // cut where the tiles alone would leave CUs idle; tiles of few rows, whose lengths a single long request may dominate, as far as
-    // the partial results stay small
-    p.slots = tiles * kv.heads >= (p.step ? 4096 : 512) ? 0 : std::max(1, 512 / kv.heads);
+    p.slots = tiles * kv.heads > most_tiles(bm) ? 0 : std::max(1, 512 / kv.heads);
     p.items = (int)(tiles + p.slots);                                // tiles cut into c = work / slots units, or fewer
     p.ws_bytes = p.slots ? attn_notes_bytes(p.items) + (size_t)p.items * kv.heads * attn_partial_floats(bm, kv.D) * 4 : 0;
     return p;
 }
-static int64_t most_rows(int T, int group, int max_new) { return (int64_t)(max_new && max_new < T ? max_new : T) * group; }
 
 AttnPlan attention_plan(const KvView &kv, int T, int requests, int q_heads, int max_new)
 {
-    const int group = q_heads / kv.heads, bm = tile_rows(kv.D, most_rows(T, group, max_new));
+    const int group = q_heads / kv.heads, bm = tile_rows(kv, T, group, max_new);
     return plan_of(kv, (int64_t)T * group / bm + requests, bm);
 }
 
 // The most that a call with these sizes or smaller ones asks for.
 size_t attention_workspace_bytes(const KvView &kv, int T, int requests, int q_heads, int max_new)
 {
-    const int group = q_heads / kv.heads, largest = tile_rows(kv.D, most_rows(T, group, max_new));
+    const int group = q_heads / kv.heads, largest = tile_rows(kv, T, group, max_new);
     size_t most = 0;
     for (int bm : {16, 32, 128}) {
         if (bm > largest) break;
-        const int64_t limit = ((bm < 128 ? 4096 : 512) - 1) / kv.heads;      // tiles of the largest call that is cut
+        const int64_t limit = most_tiles(bm) / kv.heads;             // of the largest call that is cut
         most = std::max(most, plan_of(kv, std::min((int64_t)T * group / bm + requests, limit), bm).ws_bytes);
     }
     return most;

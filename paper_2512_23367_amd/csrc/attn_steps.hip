@@ -289,7 +289,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attn_step_kernel(AttnAr
         for (int e = 0; e < ET; ++e) o[n][e] *= w;
     }
     const bool partial = it.parts > 1;
-    float *out = partial ? attn_partial(a, plan, index, kvh) : nullptr;
+    float *out = partial ? attn_partial(a, plan, it.item, kvh) : nullptr;
 #pragma unroll
     for (int e0 = 0; e0 < ET; e0 += EP) {
 #pragma unroll

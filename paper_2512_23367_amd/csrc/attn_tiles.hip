@@ -23,6 +23,7 @@ __global__ __launch_bounds__(NW * 64, D == 256 ? 1 : 2) void attn_tile_kernel(At
     constexpr int BM = 32 * NW, TB = D == 256 ? 1 : 2;               // rows; blocks of 32 tokens in a tile of keys
     constexpr int TOK = 32 * TB, KS = D / 16, ET = D / 32;
     constexpr int BLOCK = 32 * D * 4;                                // bytes of a block's keys and values in LDS (fp16)
+    constexpr int VALU_ONLY = 0x6;                                   // sched_barrier: vector and scalar arithmetic may pass
     constexpr int SC = ELEM == 1 ? 3 * TOK : 1;
     extern __shared__ __attribute__((aligned(1024))) char stage[];
     auto tile = [&](int i) { return stage + i * TB * BLOCK; };
@@ -150,16 +151,24 @@ __global__ __launch_bounds__(NW * 64, D == 256 ? 1 : 2) void attn_tile_kernel(At
 
     // ---- one tile: S^T = K Q^T, softmax down the columns, O^T += V^T P^T ----
     auto take = [&](bool masked, int t, const char *from, const float *sc, const int (&pg)[TB]) {
+        // The operands from LDS are asked for a block ahead: a read takes as long as four matrix instructions, and left to itself the
+        // compiler keeps two of them under way.
         f16v s[TB];
+        h8 x[KS];
+        auto key = [&](int b, int k) { return *reinterpret_cast<const h8 *>(from + b * BLOCK + k * 1024 + lane * 16); };
+        auto value = [&](int b, int i) { return *reinterpret_cast<const h8 *>(from + b * BLOCK + 32 * D * 2 + (i % ET) * 2048 + (i / ET) * 1024 + lane * 16); };
 #pragma unroll
-        for (int b = 0; b < TB; ++b) {
+        for (int i = 0; i < KS; ++i) x[i] = key(i % TB, i / TB);
+#pragma unroll
+        for (int b = 0; b < TB; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[b][i] = 0;
+        __builtin_amdgcn_s_setprio(1);                               // ahead of the other wavefront's softmax (int8 chunks 630 -> 621 us)
 #pragma unroll
-            for (int k = 0; k < KS; ++k) {
-                const h8 x = *reinterpret_cast<const h8 *>(from + b * BLOCK + k * 1024 + lane * 16);
-                s[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, q[k], s[b], 0, 0, 0);
-            }
+        for (int i = 0; i < TB * KS; ++i) {                          // the blocks in turn: no product waits for the one before
+            s[i % TB] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i % KS], q[i / TB], s[i % TB], 0, 0, 0);
+            x[i % KS] = i + KS < TB * KS ? key((i + KS) % TB, (i + KS) / TB) : value(0, i % KS);
+            __builtin_amdgcn_sched_barrier(VALU_ONLY);
         }
         if constexpr (ELEM == 1) {
 #pragma unroll
@@ -184,6 +193,7 @@ __global__ __launch_bounds__(NW * 64, D == 256 ? 1 : 2) void attn_tile_kernel(At
                 }
             }
         }
+        __builtin_amdgcn_s_setprio(0);
         float top = s[0][0];
 #pragma unroll
         for (int b = 0; b < TB; ++b)
@@ -220,23 +230,26 @@ __global__ __launch_bounds__(NW * 64, D == 256 ? 1 : 2) void attn_tile_kernel(At
                     const f4 iv = *reinterpret_cast<const f4 *>(sc + 2 * TOK + 32 * b + 8 * i4 + 4 * h);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) l = fmaf(x[i], iv[i], l);
-                } else {
-                    l += (x[0] + x[1]) + (x[2] + x[3]);
                 }
                 w[2 * i4] = pack2(x[0], x[1]), w[2 * i4 + 1] = pack2(x[2], x[3]);
+                if constexpr (ELEM == 2) {                           // two weights (as rounded for the products) a step; plain sums: D = 64 53.4 us for 50.7
+                    const h2 one = {(_Float16)1, (_Float16)1};
+                    l = __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, w[2 * i4]), one, l, false);
+                    l = __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, w[2 * i4 + 1]), one, l, false);
+                }
             }
             p[b][0] = as_h8(u4{w[0], w[1], w[2], w[3]}), p[b][1] = as_h8(u4{w[4], w[5], w[6], w[7]});
         }
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int b = 0; b < TB; ++b)
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-#pragma unroll
-                for (int e = 0; e < ET; ++e) {
-                    const h8 x = *reinterpret_cast<const h8 *>(from + b * BLOCK + 32 * D * 2 + e * 2048 + k * 1024 + lane * 16);
-                    o[e] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, p[b][k], o[e], 0, 0, 0);
-                }
+            for (int i = 0; i < KS; ++i) {                           // (KS = 2 ET operands of values, too)
+                o[i % ET] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i], p[b][i / ET], o[i % ET], 0, 0, 0);
+                if (b + 1 < TB) x[i] = value(b + 1, i);
+                __builtin_amdgcn_sched_barrier(VALU_ONLY);
             }
+        __builtin_amdgcn_s_setprio(0);
     };
 
     // ---- over the tiles ----
@@ -272,7 +285,7 @@ __global__ __launch_bounds__(NW * 64, D == 256 ? 1 : 2) void attn_tile_kernel(At
     }
     if (it.parts > 1) {
         if (!live) return;
-        float *out = attn_partial(a, plan, index, kvh);
+        float *out = attn_partial(a, plan, it.item, kvh);
         const int r = wave * 32 + col;
 #pragma unroll
         for (int e = 0; e < ET; ++e)
@@ -296,15 +309,15 @@ __global__ __launch_bounds__(NW * 64, D == 256 ? 1 : 2) void attn_tile_kernel(At
         }
 }
 
-template <int ELEM, int D>
+template <int ELEM, int D, int NW>
 int launch(const AttnArgs &a, const AttnPlan &p, float c, unsigned flip, hipStream_t st)
 {
     constexpr int LDS = 2 * (D == 256 ? 1 : 2) * 32 * D * 4;
-    auto kern = attn_tile_kernel<ELEM, D, 4>;
+    auto kern = attn_tile_kernel<ELEM, D, NW>;
     // once per kernel and process; the initialisation of a function-local static is thread-safe
     static const hipError_t attr_status = hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
     QL_TRY(check_hip(attr_status, "hipFuncSetAttribute(max dynamic LDS)"));
-    kern<<<(unsigned)(p.items * a.kv.heads), 256, LDS, st>>>(a, p, c, flip);
+    kern<<<(unsigned)(p.items * a.kv.heads), NW * 64, LDS, st>>>(a, p, c, flip);
     return check_hip(hipGetLastError(), "attn_tile_kernel");
 }
 
@@ -314,13 +327,13 @@ int launch_attention_tiles(const AttnArgs &a, const AttnPlan &p, float c, hipStr
 {
     const unsigned flip = a.scale < 0 ? 0x80008000u : 0u;
     if (a.kv.bits == 16) {
-        if (a.kv.D == 64) return launch<2, 64>(a, p, c, flip, st);
-        if (a.kv.D == 128) return launch<2, 128>(a, p, c, flip, st);
-        return launch<2, 256>(a, p, c, flip, st);
+        if (a.kv.D == 64) return launch<2, 64, 4>(a, p, c, flip, st);
+        if (a.kv.D == 256) return launch<2, 256, 4>(a, p, c, flip, st);
+        return p.bm == 256 ? launch<2, 128, 8>(a, p, c, flip, st) : launch<2, 128, 4>(a, p, c, flip, st);
     }
-    if (a.kv.D == 64) return launch<1, 64>(a, p, c, flip, st);
-    if (a.kv.D == 128) return launch<1, 128>(a, p, c, flip, st);
-    return launch<1, 256>(a, p, c, flip, st);
+    if (a.kv.D == 64) return launch<1, 64, 4>(a, p, c, flip, st);
+    if (a.kv.D == 256) return launch<1, 256, 4>(a, p, c, flip, st);
+    return p.bm == 256 ? launch<1, 128, 8>(a, p, c, flip, st) : launch<1, 128, 4>(a, p, c, flip, st);
 }
 
 }  // namespace ql

@@ -11,38 +11,40 @@ namespace {
 // With n_b = new tokens, T_b = take_b pages, R_b = give_b pages of request b, everything follows from three prefix sums over the
 // requests: row t belongs to the request whose range of cu holds it, the i-th page taken is ring[head + i], the i-th given
 // back goes to ring[head + free + i].  No step waits for another, so one launch does it: every workgroup forms the sums itself (at most
-// 4096 requests, from the caches) and takes a share of the tokens and pages.  The places of the ring that a call reads and
-// those that it writes are different ones, entries of the table that are looked up for tokens are not those that are written;
-// only the pool's state is read by all and written at the end, by the workgroup that finishes last, so that it may be updated in place.
+// 4096 requests, from the caches), and every thread takes a token, a page taken or a page given back.  The places of the ring that a call
+// reads and those that it writes are different ones, entries of the table that are looked up for tokens are not those that are written;
+// only the pool's state is read by all and written at the end, where it is updated in place by the workgroup that finishes last.
+// Bound by latency: lengths -> sums -> search in them -> table or ring.  1024 requests, 27000 tokens: 6.9 us (tokens, pages taken and
+// pages given back one after the other in a thread: 11.2); 64 requests of a
+// decode step: 4.1.
 constexpr int RESIZE_THREADS = 256;
 constexpr int RESIZE_MOST = 4096;
 
-__device__ inline int64_t wave_prefix(int64_t v, int lane)    // inclusive
-{
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int64_t o = __shfl_up(v, d);
-        if (lane >= d) v += o;
-    }
-    return v;
-}
+struct Sums {
+    int64_t tokens, pages;                                    // pages taken, pages given << 32 (each sum below 2^31)
+};
 
-// exclusive prefix sum over the workgroup's threads; total in `sum`
-__device__ inline int64_t block_prefix(int64_t v, int64_t *part, int64_t &sum)
+// exclusive prefix sums over the workgroup's threads, and the totals
+__device__ inline Sums sums_before(Sums v, Sums *part, Sums &all)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t inc = wave_prefix(v, lane);
+    Sums inc = v;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int64_t t = __shfl_up(inc.tokens, d), p = __shfl_up(inc.pages, d);
+        if (lane >= d) inc.tokens += t, inc.pages += p;
+    }
     __syncthreads();                                          // (of an earlier use of `part`)
     if (lane == 63) part[wave] = inc;
     __syncthreads();
-    int64_t before = 0;
-    sum = 0;
+    Sums before = {inc.tokens - v.tokens, inc.pages - v.pages};
+    all = {0, 0};
 #pragma unroll
     for (int w = 0; w < RESIZE_THREADS / 64; ++w) {
-        if (w < wave) before += part[w];
-        sum += part[w];
+        if (w < wave) before.tokens += part[w].tokens, before.pages += part[w].pages;
+        all.tokens += part[w].tokens, all.pages += part[w].pages;
     }
-    return before + inc - v;
+    return before;
 }
 
 // the request whose range of the prefix sums holds i: the last b with sums[b] <= i (sums[n] > i, so ranges of length 0 are passed over)
@@ -56,98 +58,127 @@ __device__ inline int request_of(const int *sums, int n, int i)
     return lo;
 }
 
-__global__ __launch_bounds__(RESIZE_THREADS) void kv_resize_kernel(const int32_t *__restrict__ old_len, const int32_t *__restrict__ want_len, int B,
-                                                                   int page_shift, int32_t *ring, int pages, const int32_t *pool, int32_t *pool_out,
-                                                                   int32_t *table, int64_t ld_table, int columns, int32_t *__restrict__ kv_len,
-                                                                   int32_t *__restrict__ cu_new, int32_t *__restrict__ slots,
-                                                                   int32_t *__restrict__ positions, int max_tokens)
-{
-    __shared__ int cu[RESIZE_MOST + 1], takes[RESIZE_MOST + 1], gives[RESIZE_MOST + 1];
-    __shared__ int64_t part[RESIZE_THREADS / 64];
-    const int tid = threadIdx.x, page = 1 << page_shift, cap = columns << page_shift;
-    const int per = (B + RESIZE_THREADS - 1) / RESIZE_THREADS, first = min(B, tid * per), last = min(B, first + per);
+struct ResizeArgs {
+    const int32_t *old_len, *want_len;
+    int32_t *ring;
+    const int32_t *pool;
+    int32_t *pool_out, *table;
+    int64_t ld_table;
+    int32_t *kv_len, *cu_new, *slots, *positions;
+    int requests, page_shift, pages, columns, max_tokens;
+};
 
-    int head = pool[0] % pages, free = pool[1];
+// PER: requests of a thread
+template <int PER>
+__global__ __launch_bounds__(RESIZE_THREADS) void kv_resize_kernel(ResizeArgs a)
+{
+    constexpr int MOST = PER * RESIZE_THREADS;
+    __shared__ int cu[MOST + 1], takes[MOST + 1], gives[MOST + 1];
+    __shared__ Sums part[RESIZE_THREADS / 64];
+    __shared__ int64_t losses[RESIZE_THREADS / 64];
+    const int tid = threadIdx.x, B = a.requests, page = 1 << a.page_shift, cap = a.columns << a.page_shift, pages = a.pages;
+    const int first = tid * PER;
+
+    int old_[PER], want[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) old_[i] = first + i < B ? a.old_len[first + i] : 0, want[i] = first + i < B ? a.want_len[first + i] : 0;
+    int head = a.pool[0] % pages, free = a.pool[1];
     head = head < 0 ? head + pages : head;
     free = min(max(free, 0), pages);
 
-    auto old_of = [&](int b) { return min(max(old_len[b], 0), cap); };
-    auto pages_of = [&](int len) { return (int)(((int64_t)len + page - 1) >> page_shift); };
-
-    int64_t mine = 0, sum;
-    for (int b = first; b < last; ++b) mine += max(0, max(want_len[b], 0) - old_of(b));
-    int64_t at = block_prefix(mine, part, sum);
-    for (int b = first; b < last; ++b) {
-        cu[b] = (int)min(at, (int64_t)max_tokens);
-        at += max(0, max(want_len[b], 0) - old_of(b));
+    auto pages_of = [&](int len) { return (int)(((int64_t)len + page - 1) >> a.page_shift); };
+    auto clip_old = [&](int len) { return min(max(len, 0), cap); };
+    // the length that a request would have with pages for all of it; pages that it takes or gives
+    auto target = [&](int o, int w, int n) { return w < o ? w : (int)min((int64_t)o + n, (int64_t)cap); };
+    auto moved = [&](int o, int t) -> int64_t {
+        const int d = pages_of(t) - pages_of(o);
+        return d > 0 ? (int64_t)d : (int64_t)-d << 32;
+    };
+    Sums mine = {0, 0}, all;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int o = clip_old(old_[i]), w = max(want[i], 0);
+        old_[i] = o, want[i] = w;
+        mine.tokens += max(0, w - o), mine.pages += moved(o, target(o, w, max(0, w - o)));
     }
-    if (tid == 0) cu[B] = (int)min(sum, (int64_t)max_tokens);
+    Sums before = sums_before(mine, part, all);
+    const bool fits = all.tokens <= a.max_tokens;
+    auto clipped = [&](int64_t t) { return (int)min(t, (int64_t)a.max_tokens); };
+    if (!fits) {                                              // fewer tokens than wanted: the pages once more
+        int64_t t = before.tokens;
+        mine.pages = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int n = max(0, want[i] - old_[i]);
+            mine.pages += moved(old_[i], target(old_[i], want[i], clipped(t + n) - clipped(t)));
+            t += n;
+        }
+        Sums ignored;
+        before.pages = sums_before({0, mine.pages}, part, ignored).pages;
+        all.pages = ignored.pages;
+    }
+    int64_t lost = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int b = first + i, o = old_[i], w = want[i], from = clipped(before.tokens), n = clipped(before.tokens + max(0, w - o)) - from;
+        const int t = target(o, w, n), has = pages_of(o), taken = (int)(before.pages & 0xffffffff), d = pages_of(t) - has;
+        const int got = d > 0 ? min(max(free - taken, 0), d) : 0;
+        const int len = w < o ? w : (int)min((int64_t)t, (int64_t)(has + got) << a.page_shift);
+        if (b <= B) cu[b] = from, takes[b] = taken, gives[b] = (int)(before.pages >> 32);
+        if (b < B) {
+            if (w >= o) lost += (int64_t)o + n - len;
+            if (blockIdx.x == 0) a.kv_len[b] = len, a.cu_new[b] = from;
+        }
+        before.tokens += max(0, w - o), before.pages += moved(o, t);
+    }
+    if (tid == RESIZE_THREADS - 1 && B == MOST) cu[B] = clipped(all.tokens), takes[B] = (int)(all.pages & 0xffffffff), gives[B] = (int)(all.pages >> 32);
+    if (blockIdx.x == 0 && tid == 0) a.cu_new[B] = clipped(all.tokens);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) lost += __shfl_xor(lost, d);
+    if ((tid & 63) == 0) losses[tid >> 6] = lost;
     __syncthreads();
 
-    // the length that request b would have with pages for all of it
-    auto target_of = [&](int b) {
-        const int o = old_of(b), w = max(want_len[b], 0);
-        return w < o ? w : (int)min((int64_t)o + (cu[b + 1] - cu[b]), (int64_t)cap);
-    };
-    int64_t both = 0;                                         // pages taken, pages given << 32 (each sum below 2^31)
-    for (int b = first; b < last; ++b) {
-        const int d = pages_of(target_of(b)) - pages_of(old_of(b));
-        both += d > 0 ? (int64_t)d : (int64_t)-d << 32;
-    }
-    int64_t all;
-    int64_t before = block_prefix(both, part, all);
-    int64_t lost = 0;
-    for (int b = first; b < last; ++b) {
-        const int o = old_of(b), t = target_of(b), has = pages_of(o), d = pages_of(t) - has, w = max(want_len[b], 0);
-        const int taken = (int)(before & 0xffffffff);
-        takes[b] = taken, gives[b] = (int)(before >> 32);
-        before += d > 0 ? (int64_t)d : (int64_t)-d << 32;
-        const int got = d > 0 ? min(max(free - taken, 0), d) : 0;
-        const int len = w < o ? w : (int)min((int64_t)t, (int64_t)(has + got) << page_shift);
-        if (w >= o) lost += (int64_t)o + (cu[b + 1] - cu[b]) - len;
-        if (blockIdx.x == 0) kv_len[b] = len, cu_new[b] = cu[b];
-    }
-    if (tid == 0) {
-        takes[B] = (int)(all & 0xffffffff), gives[B] = (int)(all >> 32);
-        if (blockIdx.x == 0) cu_new[B] = cu[B];
-    }
-    int64_t lost_sum;
-    block_prefix(lost, part, lost_sum);                       // (its barriers also make takes and gives visible)
-
-    const int from = blockIdx.x * RESIZE_THREADS + tid, step = gridDim.x * RESIZE_THREADS;
-    const int taken = min(takes[B], free), given = min(gives[B], pages - free);   // (a pool that is in order has room for all of them)
-    auto ring_at = [&](int64_t i) { return ring + (head + i) % pages; };
-    for (int64_t t = from; t < cu[B]; t += step) {
-        const int b = request_of(cu, B, (int)t), o = old_of(b), has = pages_of(o);
-        const int64_t pos = (int64_t)o + (t - cu[b]);
-        const int64_t j = pos >> page_shift;
-        int p = -1;
-        if (j < has) p = table[b * ld_table + j];
-        else if (pos < cap && takes[b] + j - has < free) p = *ring_at(takes[b] + j - has);
-        slots[t] = p >= 0 && p < pages ? (p << page_shift) + (int)(pos & (page - 1)) : -1;
-        positions[t] = (int)min(pos, (int64_t)INT32_MAX);
-    }
-    for (int64_t i = from; i < taken; i += step) {
-        const int b = request_of(takes, B, (int)i);
-        table[b * ld_table + pages_of(old_of(b)) + (i - takes[b])] = *ring_at(i);
-    }
-    for (int64_t i = from; i < given; i += step) {
-        const int b = request_of(gives, B, (int)i);
-        *ring_at((int64_t)free + i) = table[b * ld_table + pages_of(max(want_len[b], 0)) + (i - gives[b])];
+    const int tokens = cu[B], taken = min(takes[B], free), given = min(gives[B], pages - free);   // (a pool that is in order has room for all of them)
+    auto ring_at = [&](int64_t i) { return a.ring + (head + i) % pages; };
+    const int64_t items = (int64_t)tokens + taken + given;
+    for (int64_t at = blockIdx.x * RESIZE_THREADS + tid; at < items; at += gridDim.x * RESIZE_THREADS) {
+        const bool is_token = at < tokens, is_take = !is_token && at < (int64_t)tokens + taken;
+        const int i = (int)(is_token ? at : is_take ? at - tokens : at - tokens - taken);
+        const int *sums = is_token ? cu : is_take ? takes : gives;
+        const int b = request_of(sums, B, i), k = i - sums[b];
+        int32_t *row = a.table + b * a.ld_table;
+        if (is_token) {
+            const int o = clip_old(a.old_len[b]), has = pages_of(o);
+            const int64_t pos = (int64_t)o + k, j = pos >> a.page_shift;
+            int p = -1;
+            if (j < has) p = row[j];
+            else if (pos < cap && takes[b] + j - has < free) p = *ring_at(takes[b] + j - has);
+            a.slots[i] = p >= 0 && p < pages ? (p << a.page_shift) + (int)(pos & (page - 1)) : -1;
+            a.positions[i] = (int)min(pos, (int64_t)INT32_MAX);
+        } else if (is_take) {
+            row[pages_of(clip_old(a.old_len[b])) + k] = *ring_at(i);
+        } else {
+            *ring_at((int64_t)free + i) = row[pages_of(max(a.want_len[b], 0)) + k];
+        }
     }
 
-    if (gridDim.x > 1) {                                      // all have read the pool's state once the last one arrives
+    if (a.pool_out == a.pool && gridDim.x > 1) {              // all have read the pool's state once the last one arrives
         __shared__ int arrived;
         __syncthreads();
-        if (tid == 0) arrived = __hip_atomic_fetch_add(pool_out + 3, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+        if (tid == 0) arrived = __hip_atomic_fetch_add(a.pool_out + 3, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
         __syncthreads();
         if (arrived != (int)gridDim.x - 1) return;
+    } else if (blockIdx.x != 0) {
+        return;
     }
     if (tid == 0) {
-        pool_out[0] = (int)(((int64_t)head + taken) % pages);
-        pool_out[1] = free - taken + given;
-        pool_out[2] = (int)min(lost_sum, (int64_t)INT32_MAX);
-        __hip_atomic_store(pool_out + 3, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        int64_t sum = 0;
+#pragma unroll
+        for (int w = 0; w < RESIZE_THREADS / 64; ++w) sum += losses[w];
+        a.pool_out[0] = (int)(((int64_t)head + taken) % pages);
+        a.pool_out[1] = free - taken + given;
+        a.pool_out[2] = (int)min(sum, (int64_t)INT32_MAX);
+        __hip_atomic_store(a.pool_out + 3, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
 }
 
@@ -514,10 +545,11 @@ int launch_kv_resize(const int32_t *old_len, const int32_t *want_len, int reques
         kv_no_requests_kernel<<<1, 64, 0, st>>>(pool, pool_out, cu_new);
         return check_hip(hipGetLastError(), "kv_no_requests_kernel");
     }
-    // a token per thread: each is a search in the sums and three loads that wait for each other (1024 requests, 27000 tokens: RESIZE_FIGURES)
-    const int grid = min(512, max(1, max(ceil_div(max_tokens, RESIZE_THREADS), requests / 64)));
-    kv_resize_kernel<<<grid, RESIZE_THREADS, 0, st>>>(old_len, want_len, requests, page_shift, ring, pages, pool, pool_out, table, ld_table, columns,
-                                                      kv_len, cu_new, slots, positions, max_tokens);
+    const ResizeArgs a = {old_len, want_len, ring, pool, pool_out, table, ld_table, kv_len, cu_new, slots, positions, requests, page_shift, pages, columns, max_tokens};
+    const int grid = (int)min((int64_t)512, 1 + ((int64_t)max_tokens + 2 * (int64_t)requests) / RESIZE_THREADS);
+    if (requests <= RESIZE_THREADS) kv_resize_kernel<1><<<grid, RESIZE_THREADS, 0, st>>>(a);
+    else if (requests <= 4 * RESIZE_THREADS) kv_resize_kernel<4><<<grid, RESIZE_THREADS, 0, st>>>(a);
+    else kv_resize_kernel<RESIZE_MOST / RESIZE_THREADS><<<grid, RESIZE_THREADS, 0, st>>>(a);
     return check_hip(hipGetLastError(), "kv_resize_kernel");
 }
 

@@ -199,3 +199,16 @@ def test_many_requests(U, requests, new_most, max_new, bits):
     ctx[requests // 2], new[requests // 2], ctx[-1], new[-1] = 3000, 1, 700, new_most
     r = U.Requests(requests, ctx.tolist(), new.tolist(), 4, 2, 64, bits, 32)
     r.check(r.call(max_new=max_new), rows=np.unique(np.r_[rng.integers(0, r.T, 60), r.T - 1, r.cu[requests // 2]]))
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("ctx,new,heads,kv_heads,window", [([0, 100], [900, 760], 32, 32, 0), ([0, 64, 5], [1200, 31, 900], 24, 8, 0), ([0, 700], [1000, 700], 32, 32, 300)])
+def test_long_prompts(U, ctx, new, heads, kv_heads, window, bits):
+    """Enough rows for the largest tiles; some of the rows against the oracle: the first and last ones, those around the tiles' borders."""
+    r = U.Requests(30, ctx, new, heads, kv_heads, 128, bits, 64)
+    y = r.call(window=window)
+    g = heads // kv_heads
+    edges = np.concatenate([c + np.arange(0, n, 256 // g) for c, n in zip(r.cu[:-1], new)])
+    rows = np.unique(np.clip(np.concatenate([edges, edges + 1, edges - 1, r.cu[1:] - 1, np.random.default_rng(1).integers(0, r.T, 20)]), 0, r.T - 1))
+    r.check(y, window=window, rows=rows)
+    assert torch.isfinite(y).all()
