@@ -336,9 +336,8 @@ __global__ __launch_bounds__(2 * D) void kv_append_kernel(AppendArgs a)
     auto table_row = [&](int t) { return a.cos_sin + (int64_t)min(max(a.positions[t], 0), a.max_positions - 1) * a.rotary; };
 
     if ((int)blockIdx.x >= a.kv_groups) {                 // queries: 32 (token, head) pairs
-        const int64_t pair = (int64_t)(blockIdx.x - a.kv_groups) * 32 + tid / LANES;
-        const int t = (int)(pair / a.q_heads), head = (int)(pair % a.q_heads);
-        if (t >= a.T) return;
+        const unsigned pair = (blockIdx.x - (unsigned)a.kv_groups) * 32u + tid / LANES, t = pair / (unsigned)a.q_heads, head = pair - t * (unsigned)a.q_heads;
+        if (t >= (unsigned)a.T) return;
         const Turn u(tid % LANES, a.rotary);
         const __half *src = a.q + t * a.ldq + (int64_t)head * D;
         __half *dst = a.q_out + t * a.ldqo + (int64_t)head * D;
@@ -445,6 +444,12 @@ __global__ __launch_bounds__(2 * D) void kv_read_kernel(KvView kv, const int32_t
     const Rows rows = find_rows<TILE>(slots, t0, T, kv);
     if (tid < 64) find_pieces<ELEM>(p, rows);
     __syncthreads();
+    auto scale_of = [&](const char *block, int token, int which) { return reinterpret_cast<const float *>(block + kv_scale_offset(D))[which * KV_BLOCK + token]; };
+    float first_scale = 0;                                // of the values of this thread's first row: under way with them
+    if (ELEM == 1 && v && tid / LANES < rows.n) {
+        const int slot = p.slot[tid / LANES], rest = slot & (kv.page_size() - 1);
+        if (slot >= 0) first_scale = scale_of(kv.block(slot >> kv.page_shift, head, rest), rest % KV_BLOCK, 1);
+    }
     const int c = tid % D;
     if (v) {
         const int count = p.count;
@@ -515,13 +520,13 @@ __global__ __launch_bounds__(2 * D) void kv_read_kernel(KvView kv, const int32_t
     const int64_t column = (int64_t)head * D + 16 * j;
     if (k)
         each_row([&](int, bool there, const char *block, int token, int t) {
-            const float scale = ELEM == 1 && there ? reinterpret_cast<const float *>(block + kv_scale_offset(D))[token] : 0.f;
+            const float scale = ELEM == 1 && there ? scale_of(block, token, 0) : 0.f;
             store(k + t * ldk + column, there, block + kv_key_offset<ELEM>(token, 16 * j), 512, scale);
         });
     if (v) {
         __syncthreads();
         each_row([&](int r, bool there, const char *block, int token, int t) {
-            const float scale = ELEM == 1 && there ? reinterpret_cast<const float *>(block + kv_scale_offset(D))[KV_BLOCK + token] : 0.f;
+            const float scale = ELEM == 1 && there ? (r < 32 ? first_scale : scale_of(block, token, 1)) : 0.f;
             store(v + t * ldv + column, there, values + r * ROW + 16 * j * ELEM, 16, scale);
         });
     }
@@ -575,7 +580,7 @@ int launch_kv_append(const __half *q, int64_t ldq, const __half *k, int64_t ldk,
 {
     const int tile = tile_rows(T);
     const int64_t pairs = (int64_t)T * q_heads, kv_groups = (int64_t)ceil_div(T, tile) * kv.heads, grid = kv_groups + (pairs + 31) / 32;
-    if (grid >= (int64_t)1 << 31) return fail(QL_ERR_UNSUPPORTED, "%d tokens of %d and %d heads are more than a launch holds", T, q_heads, kv.heads);
+    if (grid >= (int64_t)1 << 31 || pairs >= ((int64_t)1 << 32) - 64) return fail(QL_ERR_UNSUPPORTED, "%d tokens of %d and %d heads are more than a launch holds", T, q_heads, kv.heads);
     const AppendArgs a = {q, k, v, ldq, ldk, ldv, ldqo, q_out, cos_sin, positions, slots, T, q_heads, rotary, max_positions, (int)kv_groups, kv};
 #define QL_CALL(E, D)                                                                 \
     do {                                                                              \
