@@ -144,6 +144,17 @@ __device__ inline bool attn_item(const AttnArgs &a, int slots, int item, AttnScr
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     constexpr int NW = THREADS / 64;
+    if (a.requests == 1) {                                   // the same without sums over lanes (one token on 300 7.0 -> 6.6 us, on 8000 14.4 -> 13.6)
+        out.r = attn_span(a, 0), out.b = 0, out.parts = 1;
+        const int tiles = attn_tiles(out.r, bm), units = attn_units(out.r.low, out.r.high);
+        if (slots) {
+            auto count = [&](float c) { return (float)tiles * (float)attn_parts(units, c); };
+            out.parts = attn_parts(units, attn_part_units<bm>((float)tiles, (float)tiles * (float)units, (float)units, slots, count));
+        }
+        out.item = (int)min((int64_t)tiles * out.parts, (int64_t)1 << 24) - 1 - item;
+        out.tile = out.item / out.parts, out.part = out.item % out.parts;
+        return out.item >= 0;
+    }
     if (a.requests <= 64) {
         AttnSpan r = {};
         if (lane < a.requests) r = attn_span(a, lane);

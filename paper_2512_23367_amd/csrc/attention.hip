@@ -15,16 +15,24 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, AttnPlan pla
     constexpr int N = D / 64;
     typedef float fn __attribute__((ext_vector_type(N)));
     const int kvh = blockIdx.x % a.kv.heads, item = blockIdx.x / a.kv.heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const size_t step = (size_t)a.kv.heads * attn_partial_floats(plan.bm, D);
+    const float *p0 = attn_partial(a, plan, item, kvh);
+    // maximum and sum of part `lane` of the first row: asked for together with the note, which says whether there is one (one token on
+    // 8000 14.4 -> 14.0 us)
+    const int first = blockIdx.y * rows + wave;
+    const float *pf = p0 + (size_t)plan.bm * D + first + min(lane, plan.items - 1 - item) * step;
+    const float m0 = pf[0], l0 = pf[plan.bm];
     const int4 note = static_cast<const int4 *>(a.ws)[item];
     const int parts = min(note.x, plan.items - item);
     if (parts < 2) return;
-    const size_t step = (size_t)a.kv.heads * attn_partial_floats(plan.bm, D);
-    for (int at = blockIdx.y * rows + wave; at < min((int)(blockIdx.y + 1) * rows, plan.bm); at += 4) {
+    for (int at = first; at < min((int)(blockIdx.y + 1) * rows, plan.bm); at += 4) {
         const int row = note.z + at;
         if (row >= note.w) return;
-        const float *p0 = attn_partial(a, plan, item, kvh), *pm = p0 + (size_t)plan.bm * D + at, *ps = p0 + (size_t)at * D + lane * N;
+        const float *pm = p0 + (size_t)plan.bm * D + at, *ps = p0 + (size_t)at * D + lane * N;
+        auto most = [&](int k) { return k == lane && at == first ? m0 : pm[k * step]; };
+        auto sum = [&](int k) { return k == lane && at == first ? l0 : pm[k * step + plan.bm]; };
         float m = -INFINITY;
-        for (int k = lane; k < parts; k += 64) m = fmaxf(m, pm[k * step]);
+        for (int k = lane; k < parts; k += 64) m = fmaxf(m, most(k));
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
         float l = 0, o[N];
@@ -32,8 +40,8 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, AttnPlan pla
         for (int i = 0; i < N; ++i) o[i] = 0;
         for (int k0 = 0; k0 < parts; k0 += 64) {
             const int k = k0 + lane;
-            const float lk = k < parts ? pm[k * step + plan.bm] : 0.f;
-            const float w = lk == 0.f ? 0.f : __builtin_amdgcn_exp2f(pm[k * step] - m);   // (lk 0: nothing seen, its sums are 0; NaN stays)
+            const float lk = k < parts ? sum(k) : 0.f;
+            const float w = lk == 0.f ? 0.f : __builtin_amdgcn_exp2f(most(k) - m);   // (lk 0: nothing seen, its sums are 0; NaN stays)
             l += lk * w;
             for (int i0 = 0; i0 < min(parts - k0, 64); i0 += 8) {             // (behind the last part: the last one again, with weight 0)
                 fn v[8];
@@ -64,7 +72,7 @@ constexpr int SHORT = 1024;
 // Rows of a tile for requests of at most `rows` rows.  Fewer than 128: the kernel for few rows.  D = 256 leaves it registers for 16.
 // 256 rows: keys and values come to a CU once for all eight of its wavefronts instead of once for every four, whose every load costs
 // the instruction issue of ten vector operations; where there are such tiles for three CUs in four.
-// us, 128 / 256 rows, 32 + 8 heads: 16384 tokens fp16 2190 / 2080; 2 x 2048 on 9000 627 / 680; 4096, 32 + 32 heads, 171 / 151, int8 191 / 165;
+// us, 128 / 256 rows, 32 + 8 heads: 16384 tokens fp16 2190 / 2080; 2 x 1000 on 9000 and 17000 int8 680 / 627; 4096, 32 + 32 heads, 171 / 151, int8 191 / 165;
 // 2048, 12 + 12 heads (108 tiles of 256) 52 / 52; D = 64, 8192 tokens int8 398 / 430.
 static int tile_rows(const KvView &kv, int T, int group, int max_new)
 {
