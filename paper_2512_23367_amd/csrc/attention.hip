@@ -93,6 +93,7 @@ static AttnPlan plan_of(const KvView &kv, int64_t tiles, int bm)
     p.bm = bm, p.step = bm < 128;
     p.slots = tiles * kv.heads > most_tiles(bm) ? 0 : std::max(1, 512 / kv.heads);
     p.items = (int)(tiles + p.slots);                                // tiles cut into c = work / slots units, or fewer
+    p.far_first = !p.step && !p.slots && (int64_t)p.items * kv.heads <= 2048;
     p.ws_bytes = p.slots ? attn_notes_bytes(p.items) + (size_t)p.items * kv.heads * attn_partial_floats(bm, kv.D) * 4 : 0;
     return p;
 }

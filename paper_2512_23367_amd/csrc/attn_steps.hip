@@ -141,7 +141,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attn_step_kernel(AttnAr
     }
     for (int i = 0; i < turns; ++i) {
         const int t = token_of(i);
-        bool plain = t + TOK <= high && (!a.causal || (t + TOK - 1 <= pos0 && (!a.window || t > pos1 - a.window)));
+        bool plain = t <= high - TOK && (!a.causal || (t + TOK - 1 <= pos0 && (!a.window || t > pos1 - a.window)));
         int page[PG];
 #pragma unroll
         for (int b = 0; b < PG; ++b) page[b] = page_of(i, b), plain = plain && page[b] >= 0;

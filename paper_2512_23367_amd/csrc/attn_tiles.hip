@@ -67,15 +67,24 @@ __global__ __launch_bounds__(NW * 64, D == 256 ? 1 : 2) void attn_tile_kernel(At
         for (int i = 0; i < 16; ++i) o[e][i] = 0;
     float m = -INFINITY, l = 0;
 
+    // the table's entries of 64 tiles at a time, one per lane (a load for every tile: 8192 tokens, D = 64, 339 us, so 336)
     const int32_t *row_of_table = a.table + (int64_t)it.b * a.ld_table;
-    auto entry = [&](int t) { return row_of_table[t < high ? t >> a.kv.page_shift : 0]; };
-    auto page_of = [&](int entry, int t) {                           // page of token t, -1: none
-        const int p = __builtin_amdgcn_readfirstlane(entry);
-        return t < high && (unsigned)p < (unsigned)a.kv.pages ? p : -1;
+    int entries[TB], shift = a.kv.page_shift;
+    asm("" : "+v"(shift));                                           // (a copy for the lanes, or the scalar one moves there, too)
+    auto look_up = [&](int first) {
+#pragma unroll
+        for (int i = 0; i < TB; ++i) {
+            const int64_t t = low + (int64_t)(first + lane) * TOK + 32 * i;
+            entries[i] = t < high ? row_of_table[t >> shift] : -1;
+        }
+    };
+    auto page_of = [&](int turn, int i) {                            // of block i of a tile, -1: none
+        const int p = __builtin_amdgcn_readlane(entries[i], turn & 63);
+        return (unsigned)p < (unsigned)a.kv.pages ? p : -1;
     };
     auto block_at = [&](int page, int t) { return a.kv.block(max(page, 0), kvh, t & (a.kv.page_size() - 1)); };
 
-    int pages[TB], next[TB], ahead[TB];                              // of the tile at hand, of the next one; table entries of the one after it
+    int pages[TB], next[TB];                                         // of the tile at hand, of the next one
 
     // ---- a tile into LDS ----
     constexpr int PIECES = ELEM == 2 ? TB * BLOCK / 1024 / NW : TB * BLOCK / 2 / 1024 / NW;   // KB per wavefront, as stored
@@ -125,7 +134,7 @@ __global__ __launch_bounds__(NW * 64, D == 256 ? 1 : 2) void attn_tile_kernel(At
     // What lies behind the last token, or on no page, is whatever memory held: its weights are 0, but 0 times NaN is not.  fp16: values of
     // such tokens are cleared (one tile of a workgroup); int8: the reciprocal scales, codes are finite.
     auto whole = [&](int t, const int (&pg)[TB]) {
-        bool w = t + TOK <= high;
+        bool w = t <= high - TOK;
 #pragma unroll
         for (int i = 0; i < TB; ++i) w = w && pg[i] >= 0;
         return w;
@@ -185,11 +194,17 @@ __global__ __launch_bounds__(NW * 64, D == 256 ? 1 : 2) void attn_tile_kernel(At
             asm volatile("");                                        // or the compiler compares and selects for every tile
 #pragma unroll
             for (int b = 0; b < TB; ++b) {
-                const int last = pg[b] < 0 ? -1 : a.causal ? min(high - 1, pos) : high - 1, first = a.window ? pos - a.window : -1;
+                const int t0 = t + 32 * b;
+                const int last = (pg[b] < 0 ? -1 : a.causal ? min(high - 1, pos) : high - 1) - t0;
+                const int first = a.window ? max(pos - a.window, t0 - 1) - (t0 - 1) : 0;
+                // bit k: token k of the block is seen; two operations an element (comparing and selecting, four: 16384 tokens
+                // 2119 us, so 2106; D = 256, 4096 tokens, 252, 234)
+                const unsigned seen = (last < 0 ? 0u : ~0u >> (31 - min(last, 31))) & (first > 31 ? 0u : ~0u << first);
+                const unsigned mine = seen >> (4 * h);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const int tk = t + 32 * b + 8 * (i / 4) + 4 * h + i % 4;
-                    if (tk > last || tk <= first) s[b][i] = -INFINITY;
+                    const unsigned all = __builtin_amdgcn_sbfe((int)mine, 8 * (i / 4) + i % 4, 1);
+                    s[b][i] = __builtin_bit_cast(float, (__builtin_bit_cast(unsigned, (float)s[b][i]) & all) | (0xff800000u & ~all));
                 }
             }
         }
@@ -254,17 +269,19 @@ __global__ __launch_bounds__(NW * 64, D == 256 ? 1 : 2) void attn_tile_kernel(At
 
     // ---- over the tiles ----
     if (low < high) {
+        look_up(0);
 #pragma unroll
-        for (int i = 0; i < TB; ++i) next[i] = page_of(entry(low + 32 * i), low + 32 * i), ahead[i] = entry(low + TOK + 32 * i);
+        for (int i = 0; i < TB; ++i) next[i] = page_of(0, i);
         fetch(low, tile(0), next);
         settle(tile(0), scales[0]);
-        int cur = 0;
-        for (int t = low; t < high; t += TOK, cur ^= 1) {
+        const int turns = (high - low - 1) / TOK + 1;
+        for (int turn = 0; turn < turns; ++turn) {
+            const int t = low + turn * TOK, cur = turn & 1;
             __syncthreads();                                         // tile t is there, the other buffer is free
+            const bool more = turn + 1 < turns;
+            if (more && ((turn + 1) & 63) == 0) look_up(turn + 1);
 #pragma unroll
-            for (int i = 0; i < TB; ++i)
-                pages[i] = next[i], next[i] = page_of(ahead[i], t + TOK + 32 * i), ahead[i] = entry(t + 2 * TOK + 32 * i);
-            const bool more = t + TOK < high;
+            for (int i = 0; i < TB; ++i) pages[i] = next[i], next[i] = page_of(turn + 1, i);
             if (more) fetch(t + TOK, tile(cur ^ 1), next);
             if (!whole(t, pages)) clear(t, tile(cur), scales[cur], pages);
             const bool some = wrow0 < it.r.rows && (!a.causal || (t <= pos1 && (!a.window || t + TOK - 1 > pos0 - a.window)));
