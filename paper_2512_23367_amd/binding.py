@@ -529,6 +529,8 @@ def ql_kv_append(q, k, v, cos_sin, positions, slots, q_out, cache, fmt):
         q_heads = _heads_of(q, "q", T, fmt.head_dim)
         if q_out is None or q_out.shape != q.shape or _heads_of(q_out, "q_out", T, fmt.head_dim) != q_heads:
             raise ValueError("q_out must have q's shape")
+        if T == 0:                                        # (no rows have no address, which would mean no q)
+            q, q_out, q_heads = None, None, 0
     _check(lib().ql_kv_append(_p(q), _row_stride(q) if q is not None else 0, k.data_ptr(), _row_stride(k), v.data_ptr(), _row_stride(v), T, q_heads,
                               _p(cos_sin), rotary, most, _p(positions), _ints(slots, "slots", T), _p(q_out),
                               _row_stride(q_out) if q_out is not None else 0, _cache(cache, fmt), ctypes.byref(fmt), _stream()))

@@ -291,7 +291,8 @@ __device__ inline float *attn_partial(const AttnArgs &a, const AttnPlan &p, int6
 template <int THREADS, int BM>
 __device__ inline bool attn_take(const AttnArgs &a, const AttnPlan &p, int index, int kvh, AttnScratch &s, AttnItem &it)
 {
-    const bool there = attn_item<THREADS, BM>(a, p.slots, p.far_first, index, s, it);
+    bool there = attn_item<THREADS, BM>(a, p.slots, p.far_first, index, s, it);
+    if (p.slots && there && it.item >= p.items) there = false;       // (a cu_new that decreases: more than the workspace has room for)
     if (p.slots && kvh == 0 && threadIdx.x == 0)
         static_cast<int4 *>(a.ws)[there ? it.item : index] = there && it.part == 0 && it.parts > 1 ? make_int4(it.parts, it.r.cu, it.tile * BM, it.r.rows) : make_int4(0, 0, 0, 0);
     return there;

@@ -108,6 +108,10 @@ int ql_kv_resize(const int32_t *old_len, const int32_t *want_len, int requests, 
     QL_TRY(check_ints(pool_out, "pool_out"));
     QL_TRY(check_ints(cu_new, "cu_new"));
     QL_TRY(check_ints(ring, "ring"));
+    if (max_tokens) {
+        QL_TRY(check_ints(slots, "slots"));
+        QL_TRY(check_ints(positions, "positions"));
+    }
     if (requests) {
         QL_TRY(check_ints(old_len, "old_len"));
         QL_TRY(check_ints(want_len, "want_len"));
@@ -115,14 +119,12 @@ int ql_kv_resize(const int32_t *old_len, const int32_t *want_len, int requests, 
         QL_TRY(check_ints(kv_len, "kv_len"));
         if (ld_table < columns) return fail(QL_ERR_SHAPE, "ld_table=%lld is less than columns=%d", (long long)ld_table, columns);
         const size_t n = 4 * (size_t)requests;
-        if (bytes_overlap(kv_len, n, old_len, n) || bytes_overlap(kv_len, n, want_len, n))
-            return fail(QL_ERR_UNSUPPORTED, "kv_len may not overlap old_len or want_len");
+        const size_t most = 4 * (size_t)max_tokens;
+        auto meets = [&](const void *p, size_t bytes) { return bytes_overlap(p, bytes, old_len, n) || bytes_overlap(p, bytes, want_len, n); };
+        if (meets(kv_len, n) || meets(cu_new, n + 4) || (most && (meets(slots, most) || meets(positions, most))))
+            return fail(QL_ERR_UNSUPPORTED, "kv_len, cu_new, slots and positions may not overlap old_len or want_len");
     }
     if (pool_out != pool && bytes_overlap(pool, 16, pool_out, 16)) return fail(QL_ERR_UNSUPPORTED, "pool_out is pool or does not overlap it");
-    if (max_tokens) {
-        QL_TRY(check_ints(slots, "slots"));
-        QL_TRY(check_ints(positions, "positions"));
-    }
     return launch_kv_resize(old_len, want_len, requests, __builtin_ctz(page_size), ring, pages, pool, pool_out, block_table, ld_table, columns,
                             kv_len, cu_new, slots, positions, max_tokens, static_cast<hipStream_t>(stream));
 }

@@ -137,6 +137,9 @@ class PagedDecoderLayer(DecoderLayerLinears):
         Returns fp16 [M,d], a view of an internal buffer that the next call overwrites."""
         M, D = x.shape[0], self.fmt.head_dim
         assert M <= min(self.max_tokens, requests.max_tokens) and requests.max_requests <= self.max_requests and x.shape[1] == self.d
+        assert (requests.fmt.page_size, requests.fmt.pages) == (self.fmt.page_size, self.fmt.pages)
+        if M == 0:
+            return self.y[:0]
         y_qkv, y_attention = self.y_qkv[:M], self.y_attention[:M]
         self._linear(x, "qkv", y_qkv)
         nq, nk = self.q_heads * D, self.fmt.heads * D

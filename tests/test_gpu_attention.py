@@ -212,3 +212,17 @@ def test_long_prompts(U, ctx, new, heads, kv_heads, window, bits):
     rows = np.unique(np.clip(np.concatenate([edges, edges + 1, edges - 1, r.cu[1:] - 1, np.random.default_rng(1).integers(0, r.T, 20)]), 0, r.T - 1))
     r.check(y, window=window, rows=rows)
     assert torch.isfinite(y).all()
+
+
+@pytest.mark.parametrize("max_new", [1, 0])
+def test_first_rows_that_decrease_stay_inside_the_workspace(U, max_new):
+    """cu_new [0, T, 0, T, ...] makes more of the workspace's items than the sizes allow for: the rest is left out, nothing behind it written."""
+    r = U.Requests(6, [1500] * 60, [16] * 60, 8, 2, 128, 8, 64)
+    need = ql.ql_paged_attention_bytes(r.fmt, r.T, 60, r.heads, max_new)
+    room = torch.full((need + (4 << 20),), 0xA5, dtype=torch.uint8, device=U.DEV)
+    q = U.dev(r.q)
+    y = torch.full((r.T + 64, q.shape[1]), 5.0, dtype=torch.float16, device=U.DEV)
+    cu = U.ints([0, r.T] * 30 + [0])
+    ql.ql_paged_attention(q, r.cache, r.fmt, U.ints(r.table), cu, U.ints(r.ctx), U.ints(r.len), r.D ** -0.5, y[:r.T], room[:need], max_new=max_new)
+    torch.cuda.synchronize()
+    assert bool((room[need:] == 0xA5).all()) and bool((y[r.T:] == 5).all())

@@ -190,3 +190,16 @@ def test_a_smaller_workspace_serves_smaller_calls(U):
     ws = torch.full((ql.ql_paged_attention_bytes(r.fmt, 500, 30, 8),), 0xFF, dtype=torch.uint8, device=U.DEV)
     for max_new in (0, 1, 9, 400):
         r.check(r.call(ws=ws, max_new=max_new))
+
+
+def test_a_step_without_new_tokens_and_formats_that_differ(U):
+    fmt = ql.QlKvFormat(heads=2, head_dim=64, page_size=32, pages=8, bits=8)
+    layer, _, _ = _layer(U, fmt, 4, 256, 512, 8, 16, 3)
+    cache = torch.empty(ql.ql_kv_cache_bytes(fmt), dtype=torch.uint8, device=U.DEV)
+    requests = PagedRequests(fmt, 3, 4, 16)
+    requests.step(U.ints([0, 0, 0]))
+    assert layer.forward(torch.empty((0, 256), dtype=torch.float16, device=U.DEV), requests, cache).shape == (0, 256)
+    assert requests.kv_len.tolist() == [0, 0, 0] and requests.pool.tolist() == [0, 8, 0, 0]
+    other = PagedRequests(ql.QlKvFormat(heads=2, head_dim=64, page_size=64, pages=4, bits=8), 3, 4, 16)
+    with pytest.raises(AssertionError):
+        layer.forward(torch.empty((1, 256), dtype=torch.float16, device=U.DEV), other, cache)

@@ -111,3 +111,8 @@ def test_binding_checks_tensors_on_the_host():
                  lambda: ql.ql_paged_attention(half, cache, f, i32.view(2, 4), i32, i32, i32, 1.0, half)):
         with pytest.raises((ValueError, RuntimeError, AssertionError)):
             call()
+
+
+@pytest.mark.parametrize("bad", [dict(cu=vp(0x100C)), dict(cu=vp(0x2000 - 16)), dict(slots=vp(0x2008)), dict(positions=vp(0x1000 - 60))])
+def test_resize_refuses_outputs_over_the_lengths(bad):
+    assert ql.lib().ql_kv_resize(*{**RESIZE, **bad}.values(), None) == UNSUPPORTED
