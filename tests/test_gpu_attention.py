@@ -226,3 +226,20 @@ def test_first_rows_that_decrease_stay_inside_the_workspace(U, max_new):
     ql.ql_paged_attention(q, r.cache, r.fmt, U.ints(r.table), cu, U.ints(r.ctx), U.ints(r.len), r.D ** -0.5, y[:r.T], room[:need], max_new=max_new)
     torch.cuda.synchronize()
     assert bool((room[need:] == 0xA5).all()) and bool((y[r.T:] == 5).all())
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("causal,window", [(True, 0), (True, 150), (False, 0)])
+@pytest.mark.parametrize("ctx,new,kv_heads", [([0, 500, 3, 100, 0, 40], [400, 1, 0, 700, 129, 270], 32), ([7 * i % 90 for i in range(50)], [11 * i % 61 for i in range(50)], 64)])
+def test_whole_tiles_of_ragged_requests(U, ctx, new, kv_heads, causal, window, bits):
+    """More tiles than are cut into parts, in either order in which workgroups take them."""
+    r = U.Requests(7, ctx, new, kv_heads, kv_heads, 64, bits, 32)
+    r.check(r.call(causal=causal, window=window), causal=causal, window=window)
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+def test_whole_tiles_over_long_contexts(U, bits):
+    """More than 64 tiles of tokens for one workgroup, whose table entries are looked up 64 tiles at a time."""
+    r = U.Requests(8, [4500, 90], [520, 600], 64, 64, 64, bits, 32)
+    rows = np.unique(np.r_[0, 127, 128, 519, 520, 647, 1119, np.random.default_rng(8).integers(0, r.T, 12)])
+    r.check(r.call(), rows=rows)
