@@ -37,6 +37,8 @@ struct AttnItem {
     AttnSpan r;
     int b, tile, part, parts;
     int item;                            // its number: parts of a tile follow each other
+    int ordinal;                         // of the tile, over all requests (with parts only); where there is no item left, one behind the last
+                                         // for each workgroup too many
 };
 
 __device__ inline AttnSpan attn_span(const AttnArgs &a, int b)
@@ -89,12 +91,18 @@ __device__ inline int wave_most(int v) { return wave_all(v, [](int a, int b) { r
 // Decode steps, 8 heads, int8, cut into work / slots units for 512 and for 256 workgroups (a few CUs get one more than the others): four
 // requests of 60000..131072 tokens 184, 193 us, this way 157; 32 requests of 200..4096 tokens 40, 37 us, this way 35; four new tokens
 // each (32 rows) on four requests of 30000..60000: one workgroup a CU 139 us, two 114.
+// Tiles of 128 rows are bound by the matrix instructions and by latency, and their partial results weigh more: TIMES
 template <int bm, typename COUNT>
-__device__ inline float attn_part_units(float tiles, float work, float most, int slots, COUNT parts_of_all)
+__device__ inline float attn_part_units(const KvView &kv, float tiles, float work, float most, int slots, COUNT parts_of_all)
 {
     const float least = (float)ATTN_LEAST, half = (float)max(slots / 2, 1);
     auto average = [&](float n) { return fmaxf(work * __builtin_amdgcn_rcpf(n) * 1.00001f, least); };
-    float best = average((float)slots), best_time = INFINITY;
+    const float D = (float)kv.D, unit = fmaxf(1.3f, 0.0145f * D);
+    auto tile_time = [&](float units, float n) {                     // us
+        const bool one = n <= half;
+        return kv.D == 256 ? (one ? 1.0f : 2.0f) * (4 + unit * units) : 4 + unit * (one ? 1.0f : 1.2f) * units;
+    };
+    float best = bm >= 128 ? most : average((float)slots), best_time = bm >= 128 ? tile_time(most, tiles) : INFINITY;
     for (int r = 1; r <= 2; ++r) {
         const float room = r * half;
         if (tiles > room) continue;
@@ -105,7 +113,8 @@ __device__ inline float attn_part_units(float tiles, float work, float most, int
             c *= fmaxf(n * __builtin_amdgcn_rcpf(room), 1.04f);
         }
         const float per = fminf(c, most);
-        const float time = fmaxf(1.5f * work, (r == 2 ? 2.0f : bm == 16 ? 1.33f : 2.25f) * per * half) + 2 * r * half;
+        const float time = bm >= 128 ? tile_time(per, n) + 4 + 2.4e-4f * D * n * (float)kv.heads
+                                     : fmaxf(1.5f * work, (r == 2 ? 2.0f : bm == 16 ? 1.33f : 2.25f) * per * half) + 2 * r * half;
         if (n <= room && time < best_time) best = c, best_time = time;
     }
     return best;
@@ -131,9 +140,9 @@ __device__ inline int wave_sum_before(int v, int lane)
 }
 
 struct AttnScratch {
-    int64_t part[ATTN_THREADS / 64];
+    int64_t part[ATTN_THREADS / 64], tiles[ATTN_THREADS / 64];
     float work[ATTN_THREADS / 64];
-    int64_t found[2];
+    int64_t found[3];
 };
 
 // The workgroup's tile (and part): the last of all requests first, as causal tiles get longer towards the end of a request and the longest
@@ -149,10 +158,12 @@ __device__ inline bool attn_item(const AttnArgs &a, int slots, bool far_first, i
         const int tiles = attn_tiles(out.r, bm), units = attn_units(out.r.low, out.r.high);
         if (slots) {
             auto count = [&](float c) { return (float)tiles * (float)attn_parts(units, c); };
-            out.parts = attn_parts(units, attn_part_units<bm>((float)tiles, (float)tiles * (float)units, (float)units, slots, count));
+            out.parts = attn_parts(units, attn_part_units<bm>(a.kv, (float)tiles, (float)tiles * (float)units, (float)units, slots, count));
         }
-        out.item = (int)min((int64_t)tiles * out.parts, (int64_t)1 << 24) - 1 - item;
+        const int all = (int)min((int64_t)tiles * out.parts, (int64_t)1 << 24);
+        out.item = all - 1 - item;
         out.tile = out.item / out.parts, out.part = out.item % out.parts;
+        out.ordinal = out.item >= 0 ? out.tile : tiles + item - all;
         return out.item >= 0;
     }
     if (a.requests <= 64) {
@@ -184,20 +195,22 @@ __device__ inline bool attn_item(const AttnArgs &a, int slots, bool far_first, i
         if (slots) {
             const int all = wave_total(tiles);               // (2^24 each at most)
             auto count = [&](float c) { return wave_total((float)tiles * (float)attn_parts(units, c)); };
-            const float c = attn_part_units<bm>((float)all, wave_total((float)tiles * (float)units), (float)wave_most(units), slots, count);
+            const float c = attn_part_units<bm>(a.kv, (float)all, wave_total((float)tiles * (float)units), (float)wave_most(units), slots, count);
             parts = attn_parts(units, c);
         }
         // (at most 2^24 each: more is a cu_new that decreases somewhere)
         const int n = lane < a.requests ? (int)min((int64_t)tiles * parts, (int64_t)1 << 24) : 0;
-        const int upto = wave_sum_before(n, lane);
+        const int upto = wave_sum_before(n, lane), tiles_upto = slots ? wave_sum_before(tiles, lane) : 0;
         item = __builtin_amdgcn_readlane(upto, 63) - 1 - item;
         const uint64_t owner = __ballot(item >= 0 && item < upto);
+        out.ordinal = __builtin_amdgcn_readlane(tiles_upto, 63) - 1 - item;
         if (!owner) return false;
         out.b = __builtin_ctzll(owner);
         out.r = {of(r.cu), of(r.rows), of(r.ctx), of(r.len), of(r.low), of(r.high)};
         out.parts = of(parts);
         const int k = item - (of(upto) - of(n));
         out.tile = k / out.parts, out.part = k % out.parts, out.item = item;
+        out.ordinal = of(tiles_upto) - of(tiles) + out.tile;
         return true;
     }
     int64_t tiles = 0;
@@ -214,30 +227,33 @@ __device__ inline bool attn_item(const AttnArgs &a, int slots, bool far_first, i
     tiles = 0, work = 0;
 #pragma unroll
     for (int w = 0; w < NW; ++w) tiles += s.part[w], work += s.work[w];
-    const float c = slots ? fmaxf(work * __builtin_amdgcn_rcpf((float)slots) * 1.00001f, (float)ATTN_LEAST) : 0.f;   // the average
-    int64_t want = item, before = 0;
+    const float c = slots ? fmaxf(work * __builtin_amdgcn_rcpf((float)slots) * 1.00001f, (float)(bm >= 128 ? 4 * ATTN_LEAST : ATTN_LEAST)) : 0.f;   // the average
+    int64_t want = item, before = 0, tiles_before = 0;
     if (slots == 0) want = tiles - 1 - item;
     for (int base = 0; base < a.requests && before <= want; base += THREADS) {
         const int b = base + threadIdx.x;
-        int64_t n = 0;
+        int64_t n = 0, own = 0;
+        int parts = 1;
         if (b < a.requests) {
             const AttnSpan r = attn_span(a, b);
-            n = (int64_t)attn_tiles(r, bm) * (slots ? attn_parts(attn_units(r.low, r.high), c) : 1);
+            if (slots) parts = attn_parts(attn_units(r.low, r.high), c);
+            own = attn_tiles(r, bm), n = own * parts;
         }
-        const int64_t upto = wave_sum_before(n, lane);
+        const int64_t upto = wave_sum_before(n, lane), own_upto = slots ? wave_sum_before(own, lane) : 0;
         __syncthreads();                                     // the sums of the round before have been read
-        if (lane == 63) s.part[wave] = upto;
+        if (lane == 63) s.part[wave] = upto, s.tiles[wave] = own_upto;
         __syncthreads();
-        int64_t at = before + upto - n;
+        int64_t at = before + upto - n, tile = tiles_before + own_upto - own;
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-            if (w < wave) at += s.part[w];
-            before += s.part[w];
+            if (w < wave) at += s.part[w], tile += s.tiles[w];
+            before += s.part[w], tiles_before += s.tiles[w];
         }
-        if (want >= at && want < at + n) s.found[0] = b, s.found[1] = want - at;
+        if (want >= at && want < at + n) s.found[0] = b, s.found[1] = want - at, s.found[2] = tile;
     }
     __syncthreads();
     out.b = __builtin_amdgcn_readfirstlane((int)s.found[0]);
+    out.ordinal = (int)min(tiles + item - before, (int64_t)INT32_MAX);
     if (out.b < 0) return false;
     const int k = __builtin_amdgcn_readfirstlane((int)s.found[1]);
     const AttnSpan r = attn_span(a, out.b);
@@ -245,6 +261,7 @@ __device__ inline bool attn_item(const AttnArgs &a, int slots, bool far_first, i
     out.r = {same(r.cu), same(r.rows), same(r.ctx), same(r.len), same(r.low), same(r.high)};
     out.parts = same(slots ? attn_parts(attn_units(r.low, r.high), c) : 1);
     out.tile = k / out.parts, out.part = k % out.parts, out.item = (int)want;
+    out.ordinal = __builtin_amdgcn_readfirstlane((int)s.found[2]) + out.tile;
     return true;
 }
 
@@ -266,17 +283,20 @@ __device__ inline void attn_part_range(int &low, int &high, int part, int parts)
     low = (int)min((int64_t)low + (int64_t)part * each, (int64_t)end), high = (int)min((int64_t)low + each, (int64_t)end);
 }
 
-// Workspace: for every item a note of what there is to join (int4: parts, or 0 where this item is not the first of several; first row
-// of q, first row of the tile, rows of the request), then for every item and key/value head bm rows of D fp32 sums, bm maxima (in powers
-// of two) and bm sums of the weights.
+// Workspace: for every tile a note of what there is to join, then for every item and key/value head bm rows of D fp32 sums, bm maxima (in
+// powers of two) and bm sums of the weights.
+struct alignas(16) AttnNote {
+    int parts, item;                     // of the tile (0 or 1: nothing to join), the first one's number
+    int cu, row0, rows, unused[3];       // first row of q, first row of the tile, rows of the request
+};
 __host__ __device__ inline size_t attn_partial_floats(int bm, int D) { return (size_t)bm * (D + 2); }
-__host__ __device__ inline size_t attn_notes_bytes(int items) { return ((size_t)items * 16 + 255) & ~(size_t)255; }
+__host__ __device__ inline size_t attn_notes_bytes(int tiles) { return ((size_t)tiles * sizeof(AttnNote) + 255) & ~(size_t)255; }
 
 struct AttnPlan {
     int bm;              // rows of a tile
     int step;            // 1: the kernel for few rows, whose wavefronts share a tile's tokens
     int slots;           // see attn_part_units (0: a workgroup per tile, no parts)
-    int items;           // workgroups of a key/value head
+    int tiles, items;    // tiles of a key/value head, at most, and workgroups
     int far_first;       // whole tiles in the order of what they see, over all requests: at most eight workgroups for every CU
     size_t ws_bytes;
 };
@@ -284,7 +304,7 @@ AttnPlan attention_plan(const KvView &kv, int T, int requests, int q_heads, int 
 
 __device__ inline float *attn_partial(const AttnArgs &a, const AttnPlan &p, int64_t item, int kvh)
 {
-    return reinterpret_cast<float *>(static_cast<char *>(a.ws) + attn_notes_bytes(p.items)) + (item * a.kv.heads + kvh) * attn_partial_floats(p.bm, a.kv.D);
+    return reinterpret_cast<float *>(static_cast<char *>(a.ws) + attn_notes_bytes(p.tiles)) + (item * a.kv.heads + kvh) * attn_partial_floats(p.bm, a.kv.D);
 }
 
 // Finds the workgroup's item and leaves the note of it.
@@ -293,8 +313,8 @@ __device__ inline bool attn_take(const AttnArgs &a, const AttnPlan &p, int index
 {
     bool there = attn_item<THREADS, BM>(a, p.slots, p.far_first, index, s, it);
     if (p.slots && there && it.item >= p.items) there = false;       // (a cu_new that decreases: more than the workspace has room for)
-    if (p.slots && kvh == 0 && threadIdx.x == 0)
-        static_cast<int4 *>(a.ws)[there ? it.item : index] = there && it.part == 0 && it.parts > 1 ? make_int4(it.parts, it.r.cu, it.tile * BM, it.r.rows) : make_int4(0, 0, 0, 0);
+    if (p.slots && kvh == 0 && threadIdx.x == 0 && (unsigned)it.ordinal < (unsigned)p.tiles && (!there || it.part == 0))
+        static_cast<AttnNote *>(a.ws)[it.ordinal] = there ? AttnNote{it.parts, it.item, it.r.cu, it.tile * BM, it.r.rows, {}} : AttnNote{};
     return there;
 }
 

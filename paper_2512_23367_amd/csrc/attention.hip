@@ -7,62 +7,52 @@
 namespace ql {
 namespace {
 
-// Joins the parts of the rows whose tokens several workgroups shared: a wavefront takes `rows` / 4 rows of an item and key/value head in
-// turn, its lanes the channels; the weights of the parts (lane k: part k) first, so that the loads of the sums wait for nothing.
+// Joins the parts of the rows whose tokens several workgroups shared: a thread takes 4 channels of a row, eight parts at a time with their
+// weights, all asked for at once.  Bound by latency: the note, then the parts.
 template <int D>
-__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, AttnPlan plan, int rows)
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, AttnPlan plan)
 {
-    constexpr int N = D / 64;
-    typedef float fn __attribute__((ext_vector_type(N)));
-    const int kvh = blockIdx.x % a.kv.heads, item = blockIdx.x / a.kv.heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr int LANES = D / 4, ROWS = 256 / LANES;
+    const int kvh = blockIdx.x % a.kv.heads, at = blockIdx.y * ROWS + threadIdx.x / LANES, channel = threadIdx.x % LANES * 4;
+    const AttnNote note = static_cast<const AttnNote *>(a.ws)[blockIdx.x / a.kv.heads];
+    // (where cu_new decreases a tile may have left no note: whatever is there stays inside the workspace and y)
+    const int row = note.row0 + at;
+    if (note.parts < 2 || (unsigned)note.item >= (unsigned)plan.items || row < 0 || row >= note.rows) return;
+    const int token = attn_token(a, row), parts = min(note.parts, plan.items - note.item);
+    const int64_t t = (int64_t)note.cu + token;
+    if (t < 0 || t >= a.T) return;
     const size_t step = (size_t)a.kv.heads * attn_partial_floats(plan.bm, D);
-    const float *p0 = attn_partial(a, plan, item, kvh);
-    // maximum and sum of part `lane` of the first row: asked for together with the note, which says whether there is one (one token on
-    // 8000 14.4 -> 14.0 us)
-    const int first = blockIdx.y * rows + wave;
-    const float *pf = p0 + (size_t)plan.bm * D + first + min(lane, plan.items - 1 - item) * step;
-    const float m0 = pf[0], l0 = pf[plan.bm];
-    const int4 note = static_cast<const int4 *>(a.ws)[item];
-    const int parts = min(note.x, plan.items - item);
-    if (parts < 2) return;
-    for (int at = first; at < min((int)(blockIdx.y + 1) * rows, plan.bm); at += 4) {
-        const int row = note.z + at;
-        if (row >= note.w) return;
-        const float *pm = p0 + (size_t)plan.bm * D + at, *ps = p0 + (size_t)at * D + lane * N;
-        auto most = [&](int k) { return k == lane && at == first ? m0 : pm[k * step]; };
-        auto sum = [&](int k) { return k == lane && at == first ? l0 : pm[k * step + plan.bm]; };
-        float m = -INFINITY;
-        for (int k = lane; k < parts; k += 64) m = fmaxf(m, most(k));
+    const float *p0 = attn_partial(a, plan, note.item, kvh), *pm = p0 + (size_t)plan.bm * D + at, *ps = p0 + (size_t)at * D + channel;
+    float m = -INFINITY, l = 0;
+    f4 o = {0, 0, 0, 0};
+    for (int k0 = 0; k0 < parts; k0 += 8) {
+        float mk[8], lk[8];
+        f4 v[8];
 #pragma unroll
-        for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
-        float l = 0, o[N];
-#pragma unroll
-        for (int i = 0; i < N; ++i) o[i] = 0;
-        for (int k0 = 0; k0 < parts; k0 += 64) {
-            const int k = k0 + lane;
-            const float lk = k < parts ? sum(k) : 0.f;
-            const float w = lk == 0.f ? 0.f : __builtin_amdgcn_exp2f(most(k) - m);   // (lk 0: nothing seen, its sums are 0; NaN stays)
-            l += lk * w;
-            for (int i0 = 0; i0 < min(parts - k0, 64); i0 += 8) {             // (behind the last part: the last one again, with weight 0)
-                fn v[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const fn *>(ps + min(k0 + i0 + i, parts - 1) * step);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float wi = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), i0 + i));
-#pragma unroll
-                    for (int c = 0; c < N; ++c) o[c] = fmaf(v[i][c], wi, o[c]);
-                }
-            }
+        for (int i = 0; i < 8; ++i) {                                // (behind the last part: the last one again, with weight 0)
+            const size_t off = min(k0 + i, parts - 1) * step;
+            mk[i] = pm[off], lk[i] = pm[off + plan.bm], v[i] = *reinterpret_cast<const f4 *>(ps + off);
         }
+        float top = m;
 #pragma unroll
-        for (int d = 1; d < 64; d *= 2) l += __shfl_xor(l, d);
-        const float inv = l == 0.f ? 0.f : 1.0f / l;
-        const int token = attn_token(a, row);
-        __half *dst = a.y + (int64_t)(note.y + token) * a.ldy + (int64_t)(kvh * a.group + row - token * a.group) * D + lane * N;
+        for (int i = 0; i < 8; ++i) {
+            lk[i] = k0 + i < parts ? lk[i] : 0.f;
+            top = fmaxf(top, mk[i]);
+        }
+        const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+        l *= keep, o *= keep, m = top;
 #pragma unroll
-        for (int c = 0; c < N; ++c) dst[c] = __float2half(o[c] * inv);
+        for (int i = 0; i < 8; ++i) {
+            const float w = lk[i] == 0.f ? 0.f : __builtin_amdgcn_exp2f(mk[i] - top);   // (lk 0: nothing seen, its sums are 0; NaN stays)
+            l += lk[i] * w;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) o[c] = fmaf(v[i][c], w, o[c]);
+        }
     }
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+    __half *dst = a.y + t * a.ldy + (int64_t)(kvh * a.group + row - token * a.group) * D + channel;
+    *reinterpret_cast<h4 *>(dst) = h4{(_Float16)(o[0] * inv), (_Float16)(o[1] * inv), (_Float16)(o[2] * inv), (_Float16)(o[3] * inv)};
 }
 
 constexpr int SHORT = 1024;
@@ -92,9 +82,9 @@ static AttnPlan plan_of(const KvView &kv, int64_t tiles, int bm)
     AttnPlan p = {};
     p.bm = bm, p.step = bm < 128;
     p.slots = tiles * kv.heads > most_tiles(bm) ? 0 : std::max(1, 512 / kv.heads);
-    p.items = (int)(tiles + p.slots);                                // tiles cut into c = work / slots units, or fewer
+    p.tiles = (int)tiles, p.items = (int)(tiles + p.slots);          // (no more items than that: see attn_part_units)
     p.far_first = !p.step && !p.slots && (int64_t)p.items * kv.heads <= 2048;
-    p.ws_bytes = p.slots ? attn_notes_bytes(p.items) + (size_t)p.items * kv.heads * attn_partial_floats(bm, kv.D) * 4 : 0;
+    p.ws_bytes = p.slots ? attn_notes_bytes(p.tiles) + (size_t)p.items * kv.heads * attn_partial_floats(bm, kv.D) * 4 : 0;
     return p;
 }
 
@@ -124,18 +114,17 @@ int launch_attention(const AttnArgs &a, hipStream_t st)
         if (!a.ws) return fail(QL_ERR_NULL, "ws is NULL");
         if (a.ws_bytes < p.ws_bytes) return fail(QL_ERR_WORKSPACE, "workspace has %zu bytes, this call needs %zu (see ql_paged_attention_bytes)", a.ws_bytes, p.ws_bytes);
     }
-    if (p.step && (int64_t)a.columns << a.kv.page_shift <= SHORT) p.slots = 0, p.items = (int)((int64_t)a.T * a.group / p.bm + a.requests);
+    if ((int64_t)a.columns << a.kv.page_shift <= (p.step ? SHORT : SHORT / 2)) p.slots = 0, p.items = p.tiles, p.far_first = !p.step;
     if ((int64_t)p.items * a.kv.heads >= (int64_t)1 << 31)
         return fail(QL_ERR_UNSUPPORTED, "%d tokens of %d query heads are more than a launch holds", a.T, a.q_heads);
     // exp(scale s) = exp2(c s); a scale of nothing keeps masked scores apart from the others (-inf times 0 would be NaN)
     const float c = fmaxf(std::fabs(a.scale) * 1.44269504088896341f, 1e-30f);
     QL_TRY(p.step ? launch_attention_steps(a, p, c, st) : launch_attention_tiles(a, p, c, st));
     if (!p.slots) return QL_OK;
-    const int rows = p.step ? 4 : 8;                                 // (tiles of 128 rows, 40 of them there: 4 rows 76.0 us, 8 75.5, 16 78, 32 83)
-    const dim3 grid(p.items * a.kv.heads, p.bm / rows);
-    if (a.kv.D == 64) attn_join_kernel<64><<<grid, 256, 0, st>>>(a, p, rows);
-    else if (a.kv.D == 128) attn_join_kernel<128><<<grid, 256, 0, st>>>(a, p, rows);
-    else attn_join_kernel<256><<<grid, 256, 0, st>>>(a, p, rows);
+    const dim3 grid(p.tiles * a.kv.heads, p.bm * a.kv.D / 1024);
+    if (a.kv.D == 64) attn_join_kernel<64><<<grid, 256, 0, st>>>(a, p);
+    else if (a.kv.D == 128) attn_join_kernel<128><<<grid, 256, 0, st>>>(a, p);
+    else attn_join_kernel<256><<<grid, 256, 0, st>>>(a, p);
     return check_hip(hipGetLastError(), "attn_join_kernel");
 }
 
