@@ -61,6 +61,14 @@ __device__ inline int attn_units(int low, int high) { return (max(high - low, 0)
 
 __device__ inline int attn_tiles(const AttnSpan &r, int bm) { return (r.rows + bm - 1) / bm; }
 
+// Units that a tile of the request sees, at most.
+template <int bm>
+__device__ inline int attn_tile_units(const AttnArgs &a, const AttnSpan &r)
+{
+    const int units = attn_units(r.low, r.high);
+    return a.window ? (int)min((int64_t)units, ((int64_t)a.window + attn_token(a, bm - 1) + 2 * ATTN_UNIT) / ATTN_UNIT) : units;
+}
+
 // Parts of a tile's units, of about c each (any number covers them: see attn_part_range).
 constexpr int ATTN_LEAST = 4;
 __device__ inline int attn_parts(int units, float c) { return max(1, (int)(units * __builtin_amdgcn_rcpf(c) + 0.9999f)); }
@@ -91,7 +99,9 @@ __device__ inline int wave_most(int v) { return wave_all(v, [](int a, int b) { r
 // Decode steps, 8 heads, int8, cut into work / slots units for 512 and for 256 workgroups (a few CUs get one more than the others): four
 // requests of 60000..131072 tokens 184, 193 us, this way 157; 32 requests of 200..4096 tokens 40, 37 us, this way 35; four new tokens
 // each (32 rows) on four requests of 30000..60000: one workgroup a CU 139 us, two 114.
-// Tiles of 128 rows are bound by the matrix instructions and by latency, and their partial results weigh more: TIMES
+// Tiles of 128 rows wait for themselves rather than for memory -- a unit takes a workgroup alone on its CU 1.3 us at D = 64, 1.9 at 128, 3.7
+// at 256 --, and their partial results weigh more: they are cut where that is faster by these times.  Over 120 mixed prompts and chunks 0.8 %
+// slower than the better of cutting and not cutting for each, always cutting 1.4 %, never 27 %.
 template <int bm, typename COUNT>
 __device__ inline float attn_part_units(const KvView &kv, float tiles, float work, float most, int slots, COUNT parts_of_all)
 {
@@ -113,7 +123,7 @@ __device__ inline float attn_part_units(const KvView &kv, float tiles, float wor
             c *= fmaxf(n * __builtin_amdgcn_rcpf(room), 1.04f);
         }
         const float per = fminf(c, most);
-        const float time = bm >= 128 ? tile_time(per, n) + 4 + 2.4e-4f * D * n * (float)kv.heads
+        const float time = bm >= 128 ? tile_time(per, n) + 2.5f + 1.2e-4f * D * n * (float)kv.heads
                                      : fmaxf(1.5f * work, (r == 2 ? 2.0f : bm == 16 ? 1.33f : 2.25f) * per * half) + 2 * r * half;
         if (n <= room && time < best_time) best = c, best_time = time;
     }
@@ -155,7 +165,7 @@ __device__ inline bool attn_item(const AttnArgs &a, int slots, bool far_first, i
     constexpr int NW = THREADS / 64;
     if (a.requests == 1) {                                   // the same without sums over lanes (one token on 300 7.0 -> 6.6 us, on 8000 14.4 -> 13.6)
         out.r = attn_span(a, 0), out.b = 0, out.parts = 1;
-        const int tiles = attn_tiles(out.r, bm), units = attn_units(out.r.low, out.r.high);
+        const int tiles = attn_tiles(out.r, bm), units = attn_tile_units<bm>(a, out.r);
         if (slots) {
             auto count = [&](float c) { return (float)tiles * (float)attn_parts(units, c); };
             out.parts = attn_parts(units, attn_part_units<bm>(a.kv, (float)tiles, (float)tiles * (float)units, (float)units, slots, count));
@@ -169,7 +179,7 @@ __device__ inline bool attn_item(const AttnArgs &a, int slots, bool far_first, i
     if (a.requests <= 64) {
         AttnSpan r = {};
         if (lane < a.requests) r = attn_span(a, lane);
-        const int tiles = attn_tiles(r, bm), units = attn_units(r.low, r.high);
+        const int tiles = attn_tiles(r, bm), units = attn_tile_units<bm>(a, r);
         auto of = [&](int v) { return __builtin_amdgcn_readlane(v, out.b); };
         if (bm >= 128 && far_first) {
             // By the last token that they see, counted in tiles, the farthest first: the short ones fill the end.  (Six prompts of
@@ -218,7 +228,7 @@ __device__ inline bool attn_item(const AttnArgs &a, int slots, bool far_first, i
     for (int b = threadIdx.x; b < a.requests; b += THREADS) {
         const AttnSpan r = attn_span(a, b);
         const int n = attn_tiles(r, bm);
-        tiles += n, work += (float)n * (float)attn_units(r.low, r.high);
+        tiles += n, work += (float)n * (float)attn_tile_units<bm>(a, r);
     }
     tiles = __shfl(wave_sum_before(tiles, lane), 63), work = wave_total(work);
     if (lane == 0) s.part[wave] = tiles, s.work[wave] = work;
@@ -236,7 +246,7 @@ __device__ inline bool attn_item(const AttnArgs &a, int slots, bool far_first, i
         int parts = 1;
         if (b < a.requests) {
             const AttnSpan r = attn_span(a, b);
-            if (slots) parts = attn_parts(attn_units(r.low, r.high), c);
+            if (slots) parts = attn_parts(attn_tile_units<bm>(a, r), c);
             own = attn_tiles(r, bm), n = own * parts;
         }
         const int64_t upto = wave_sum_before(n, lane), own_upto = slots ? wave_sum_before(own, lane) : 0;
@@ -259,7 +269,7 @@ __device__ inline bool attn_item(const AttnArgs &a, int slots, bool far_first, i
     const AttnSpan r = attn_span(a, out.b);
     auto same = [&](int v) { return __builtin_amdgcn_readfirstlane(v); };
     out.r = {same(r.cu), same(r.rows), same(r.ctx), same(r.len), same(r.low), same(r.high)};
-    out.parts = same(slots ? attn_parts(attn_units(r.low, r.high), c) : 1);
+    out.parts = same(slots ? attn_parts(attn_tile_units<bm>(a, r), c) : 1);
     out.tile = k / out.parts, out.part = k % out.parts, out.item = (int)want;
     out.ordinal = __builtin_amdgcn_readfirstlane((int)s.found[2]) + out.tile;
     return true;
