@@ -17,6 +17,10 @@ __device__ inline void widen_codes(unsigned w, unsigned &lo, unsigned &hi)
     hi = __builtin_bit_cast(unsigned, __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, w, 0x04030402u)) - off);
 }
 
+// Tiles that are fetched ahead, and taken between two barriers.  (us, one / two of them: eight wavefronts, fp16, 16384 tokens 2131 / 2093, int8,
+// 2 x 1000 on 9000 and 17000, 638 / 641; four wavefronts, of which two workgroups share a CU otherwise: 16 x 5 new tokens, 64 + 8 heads, 72 / 81.)
+constexpr int tile_distance(int ELEM, int NW) { return ELEM == 2 && NW == 8 ? 2 : 1; }
+
 template <int ELEM, int D, int NW>
 __global__ __launch_bounds__(NW * 64, D == 256 ? 1 : 2) void attn_tile_kernel(AttnArgs a, AttnPlan plan, float c, unsigned flip)
 {
@@ -24,10 +28,11 @@ __global__ __launch_bounds__(NW * 64, D == 256 ? 1 : 2) void attn_tile_kernel(At
     constexpr int TOK = 32 * TB, KS = D / 16, ET = D / 32;
     constexpr int BLOCK = 32 * D * 4;                                // bytes of a block's keys and values in LDS (fp16)
     constexpr int VALU_ONLY = 0x6;                                   // sched_barrier: vector and scalar arithmetic may pass
+    constexpr int DIST = tile_distance(ELEM, NW);
     constexpr int SC = ELEM == 1 ? 3 * TOK : 1;
     extern __shared__ __attribute__((aligned(1024))) char stage[];
     auto tile = [&](int i) { return stage + i * TB * BLOCK; };
-    __shared__ __attribute__((aligned(16))) float scales[2][SC];
+    __shared__ __attribute__((aligned(16))) float scales[2 * DIST][SC];
     __shared__ AttnScratch scratch;
 
     const int kvh = blockIdx.x % a.kv.heads, index = blockIdx.x / a.kv.heads;
@@ -84,7 +89,7 @@ __global__ __launch_bounds__(NW * 64, D == 256 ? 1 : 2) void attn_tile_kernel(At
     };
     auto block_at = [&](int page, int t) { return a.kv.block(max(page, 0), kvh, t & (a.kv.page_size() - 1)); };
 
-    int pages[TB], next[TB];                                         // of the tile at hand, of the next one
+    int pages[DIST + 1][TB];                                         // of the tile at hand, of the next ones
 
     // ---- a tile into LDS ----
     constexpr int PIECES = ELEM == 2 ? TB * BLOCK / 1024 / NW : TB * BLOCK / 2 / 1024 / NW;   // KB per wavefront, as stored
@@ -269,28 +274,37 @@ __global__ __launch_bounds__(NW * 64, D == 256 ? 1 : 2) void attn_tile_kernel(At
 
     // ---- over the tiles ----
     if (low < high) {
+        const int turns = (high - low - 1) / TOK + 1;
         look_up(0);
 #pragma unroll
-        for (int i = 0; i < TB; ++i) next[i] = page_of(0, i);
-        fetch(low, tile(0), next);
-        settle(tile(0), scales[0]);
-        const int turns = (high - low - 1) / TOK + 1;
-        for (int turn = 0; turn < turns; ++turn) {
-            const int t = low + turn * TOK, cur = turn & 1;
-            __syncthreads();                                         // tile t is there, the other buffer is free
-            const bool more = turn + 1 < turns;
-            if (more && ((turn + 1) & 63) == 0) look_up(turn + 1);
+        for (int d = 0; d < DIST; ++d) {
 #pragma unroll
-            for (int i = 0; i < TB; ++i) pages[i] = next[i], next[i] = page_of(turn + 1, i);
-            if (more) fetch(t + TOK, tile(cur ^ 1), next);
-            if (!whole(t, pages)) clear(t, tile(cur), scales[cur], pages);
+            for (int i = 0; i < TB; ++i) pages[d + 1][i] = page_of(d, i);
+            if (d < turns) {
+                fetch(low + d * TOK, tile(d), pages[d + 1]);
+                settle(tile(d), scales[d]);
+            }
+        }
+        for (int turn = 0; turn < turns; ++turn) {
+            const int t = low + turn * TOK, cur = turn % (2 * DIST), to = (turn + DIST) % (2 * DIST);
+            if (turn % DIST == 0) __syncthreads();                   // tiles turn .. turn + DIST - 1 are there, the other buffers free
+            const bool more = turn + DIST < turns;
+            if (more && ((turn + DIST) & 63) == 0) look_up(turn + DIST);
+#pragma unroll
+            for (int i = 0; i < TB; ++i) {
+#pragma unroll
+                for (int d = 0; d < DIST; ++d) pages[d][i] = pages[d + 1][i];
+                pages[DIST][i] = page_of(turn + DIST, i);
+            }
+            if (more) fetch(t + DIST * TOK, tile(to), pages[DIST]);
+            if (!whole(t, pages[0])) clear(t, tile(cur), scales[cur], pages[0]);
             const bool some = wrow0 < it.r.rows && (!a.causal || (t <= pos1 && (!a.window || t + TOK - 1 > pos0 - a.window)));
             if (some) {
-                bool plain = whole(t, pages);
+                bool plain = whole(t, pages[0]);
                 if (a.causal) plain = plain && t + TOK - 1 <= pos0 && (!a.window || t > pos1 - a.window);
-                take(!plain, t, tile(cur), scales[cur], pages);
+                take(!plain, t, tile(cur), scales[cur], pages[0]);
             }
-            if (more) settle(tile(cur ^ 1), scales[cur ^ 1]);
+            if (ELEM == 1 ? more : turn % DIST == DIST - 1) settle(tile(to), scales[to]);
         }
     }
 
@@ -329,7 +343,7 @@ __global__ __launch_bounds__(NW * 64, D == 256 ? 1 : 2) void attn_tile_kernel(At
 template <int ELEM, int D, int NW>
 int launch(const AttnArgs &a, const AttnPlan &p, float c, unsigned flip, hipStream_t st)
 {
-    constexpr int LDS = 2 * (D == 256 ? 1 : 2) * 32 * D * 4;
+    constexpr int LDS = 2 * tile_distance(ELEM, NW) * (D == 256 ? 1 : 2) * 32 * D * 4;
     auto kern = attn_tile_kernel<ELEM, D, NW>;
     // once per kernel and process; the initialisation of a function-local static is thread-safe
     static const hipError_t attr_status = hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
