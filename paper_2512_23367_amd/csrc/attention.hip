@@ -55,6 +55,9 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, AttnPlan pla
     *reinterpret_cast<h4 *>(dst) = h4{(_Float16)(o[0] * inv), (_Float16)(o[1] * inv), (_Float16)(o[2] * inv), (_Float16)(o[3] * inv)};
 }
 
+// Tokens that a block table can hold up to which requests of few rows are not cut into parts, which takes a second launch (tiles of 128 rows: half
+// of it).  us, whole / parts: 32 requests of one token, 8 heads, int8: on 400 tokens 8.4 / 10.3, 700 12.3 / 14.4, 1000 17.9 / 17.8; one, 12 heads:
+// 400 7.1 / 8.9, 1000 9.3 / 9.1; one of 64 new tokens, 32 + 8 heads: 60 8.5 / 10.5, 200 12.0 / 13.9, 350 15.3 / 15.0.
 constexpr int SHORT = 1024;
 
 }  // namespace

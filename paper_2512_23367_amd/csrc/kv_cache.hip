@@ -15,8 +15,7 @@ namespace {
 // reads and those that it writes are different ones, entries of the table that are looked up for tokens are not those that are written;
 // only the pool's state is read by all and written at the end, where it is updated in place by the workgroup that finishes last.
 // Bound by latency: lengths -> sums -> search in them -> table or ring.  1024 requests, 27000 tokens: 6.9 us (tokens, pages taken and
-// pages given back one after the other in a thread: 11.2); 64 requests of a
-// decode step: 4.1.
+// pages given back one after the other in a thread: 11.2); 64 requests of a decode step: 4.8.
 constexpr int RESIZE_THREADS = 256;
 constexpr int RESIZE_MOST = 4096;
 
@@ -552,6 +551,7 @@ int launch_kv_resize(const int32_t *old_len, const int32_t *want_len, int reques
     }
     const ResizeArgs a = {old_len, want_len, ring, pool, pool_out, table, ld_table, kv_len, cu_new, slots, positions, requests, page_shift, pages, columns, max_tokens};
     const int grid = (int)min((int64_t)512, 1 + ((int64_t)max_tokens + 2 * (int64_t)requests) / RESIZE_THREADS);
+    // requests of a thread: as few as hold them (64 requests 4.8 us with 1, 9.9 with 16; 1024 requests 5.9 with 4, 10.9 with 16)
     if (requests <= RESIZE_THREADS) kv_resize_kernel<1><<<grid, RESIZE_THREADS, 0, st>>>(a);
     else if (requests <= 4 * RESIZE_THREADS) kv_resize_kernel<4><<<grid, RESIZE_THREADS, 0, st>>>(a);
     else kv_resize_kernel<RESIZE_MOST / RESIZE_THREADS><<<grid, RESIZE_THREADS, 0, st>>>(a);
@@ -571,14 +571,16 @@ int launch_kv_resize(const int32_t *old_len, const int32_t *want_len, int reques
         }                                                                         \
     } while (0)
 
-// Rows of a workgroup: few tokens are mostly single ones, whose pieces are moved one after the other, and fill few workgroups.
-static int tile_rows(int T) { return T <= 256 ? 8 : 32; }
+// Rows of a workgroup: 8 where 32 would make no more than two workgroups for every CU, whose single tokens are moved one after the other.
+// Append and read back, us, 8 / 32 rows, 8 heads, int8: 128 single tokens 10.6 / 19.1; 4 requests with 512 tokens 11.6 / 14.4, 1024 13.7 / 16.9,
+// 2048 20.2 / 20.1, 4096 37 / 28; 32 heads, 512 tokens 16.7 / 18.8, 1024 22 / 20; 16000 tokens of one head 61 / 59.
+static int tile_rows(int T, int heads) { return T <= 4096 && (int64_t)T * heads <= 512 * 32 ? 8 : 32; }
 
 int launch_kv_append(const __half *q, int64_t ldq, const __half *k, int64_t ldk, const __half *v, int64_t ldv, int T, int q_heads,
                      const float *cos_sin, int rotary, int max_positions, const int32_t *positions, const int32_t *slots,
                      __half *q_out, int64_t ldqo, const KvView &kv, hipStream_t st)
 {
-    const int tile = tile_rows(T);
+    const int tile = tile_rows(T, kv.heads);
     const int64_t pairs = (int64_t)T * q_heads, kv_groups = (int64_t)ceil_div(T, tile) * kv.heads, grid = kv_groups + (pairs + 31) / 32;
     if (grid >= (int64_t)1 << 31 || pairs >= ((int64_t)1 << 32) - 64) return fail(QL_ERR_UNSUPPORTED, "%d tokens of %d and %d heads are more than a launch holds", T, q_heads, kv.heads);
     const AppendArgs a = {q, k, v, ldq, ldk, ldv, ldqo, q_out, cos_sin, positions, slots, T, q_heads, rotary, max_positions, (int)kv_groups, kv};
@@ -594,7 +596,7 @@ int launch_kv_append(const __half *q, int64_t ldq, const __half *k, int64_t ldk,
 
 int launch_kv_read(const KvView &kv, const int32_t *slots, int T, __half *k, int64_t ldk, __half *v, int64_t ldv, hipStream_t st)
 {
-    const int tile = tile_rows(T);
+    const int tile = tile_rows(T, kv.heads);
     const int64_t grid = (int64_t)ceil_div(T, tile) * kv.heads;
     if (grid >= (int64_t)1 << 31) return fail(QL_ERR_UNSUPPORTED, "%d tokens of %d heads are more than a launch holds", T, kv.heads);
 #define QL_CALL(E, D)                                                                                             \
