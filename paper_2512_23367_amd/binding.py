@@ -136,10 +136,12 @@ def _bind_native(l):
                       f"torch? rebuild with `python -m paper_2512_23367_amd.build`): {e}", RuntimeWarning)
         return
     names = ("ql_weight_bytes", "ql_act_kernel_bytes", "ql_w8a8_linear", "ql_w4a8_linear", "ql_w8a8_gemm", "ql_w4a8_gemm",
-             "ql_quant_act_per_token", "ql_quant_act_rmsnorm", "ql_quant_act_swiglu", "ql_quant_act_per_token_transformed",
-             "ql_kv_cache_bytes", "ql_kv_resize", "ql_kv_append", "ql_kv_read", "ql_paged_attention")
+             "ql_quant_act_per_token", "ql_quant_act_rmsnorm", "ql_quant_act_swiglu", "ql_quant_act_per_token_transformed")
+    cache_names = ("ql_kv_cache_bytes", "ql_kv_resize", "ql_kv_append", "ql_kv_read", "ql_paged_attention")
+    addresses = lambda names: tuple(ctypes.cast(getattr(l, n), ctypes.c_void_p).value for n in names)  # noqa: E731
+    _qlcall.bind(addresses(names))
+    _qlcall.bind_cache(addresses(cache_names))
     _qlcall.bind_format(QlKvFormat)
-    _qlcall.bind(tuple(ctypes.cast(getattr(l, n), ctypes.c_void_p).value for n in names))
     _native = _qlcall
 
 

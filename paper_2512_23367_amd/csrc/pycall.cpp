@@ -29,12 +29,15 @@ struct Library {
     decltype(&ql_quant_act_rmsnorm) quant_rmsnorm;
     decltype(&ql_quant_act_swiglu) quant_swiglu;
     decltype(&ql_quant_act_per_token_transformed) quant_transformed;
+} lib;
+
+struct CacheLibrary {
     decltype(&ql_kv_cache_bytes) kv_cache_bytes;
     decltype(&ql_kv_resize) kv_resize;
     decltype(&ql_kv_append) kv_append;
     decltype(&ql_kv_read) kv_read;
     decltype(&ql_paged_attention) paged_attention;
-} lib;
+} cache_lib;
 
 PyObject *format_type = nullptr;   // binding.py's QlKvFormat
 
@@ -354,7 +357,7 @@ void *cache_of(const Here &here, PyObject *o, const ql_kv_format &f)
 {
     size_t need = 0;
     const at::Tensor &t = here(o);
-    if (lib.kv_cache_bytes(&f, &need) != QL_OK || !t.is_contiguous() || t.nbytes() < need) throw NotPlain();
+    if (cache_lib.kv_cache_bytes(&f, &need) != QL_OK || !t.is_contiguous() || t.nbytes() < need) throw NotPlain();
     return t.data_ptr();
 }
 
@@ -378,7 +381,7 @@ PyObject *kv_resize(PyObject *, Args a, Py_ssize_t n)
         const Table t(here, a[6], requests);
         void *st = stream_from(a[11]);
         return [=] {
-            return lib.kv_resize(old_len, want, requests, page, ring, pages, pool, pool_out, t.p, t.ld, t.columns, kv_len, cu, slots, positions, most, st);
+            return cache_lib.kv_resize(old_len, want, requests, page, ring, pages, pool, pool_out, t.p, t.ld, t.columns, kv_len, cu, slots, positions, most, st);
         };
     });
 }
@@ -408,7 +411,7 @@ PyObject *kv_append(PyObject *, Args a, Py_ssize_t n)   // q, k, v, cos_sin, pos
         }
         void *cache = cache_of(here, a[7], f.f), *st = stream_from(a[9]);
         return [=] {
-            return lib.kv_append(q.p, q.ld, k.p, k.ld, v.p, v.ld, T, q.heads, cs, rotary, most, positions, slots, out.p, out.ld, cache, &f.f, st);
+            return cache_lib.kv_append(q.p, q.ld, k.p, k.ld, v.p, v.ld, T, q.heads, cs, rotary, most, positions, slots, out.p, out.ld, cache, &f.f, st);
         };
     });
 }
@@ -427,7 +430,7 @@ PyObject *kv_read(PyObject *, Args a, Py_ssize_t n)   // cache, fmt, slots, k, v
         if (v.p) v.fit(T, f.f.heads);
         const int32_t *slots = here.ints(a[2], T);
         void *cache = cache_of(here, a[0], f.f), *st = stream_from(a[5]);
-        return [=] { return lib.kv_read(cache, &f.f, slots, T, k.p, k.ld, v.p, v.ld, st); };
+        return [=] { return cache_lib.kv_read(cache, &f.f, slots, T, k.p, k.ld, v.p, v.ld, st); };
     });
 }
 
@@ -449,8 +452,8 @@ PyObject *paged_attention(PyObject *, Args a, Py_ssize_t n)
         const int causal = as_flag(a[10]), window = as_int(a[11]), most = as_int(a[12]);
         void *cache = cache_of(here, a[1], f.f), *st = stream_from(a[13]);
         return [=] {
-            return lib.paged_attention(q.p, q.ld, q.rows, q.heads, cache, &f.f, t.p, t.ld, t.columns, cu, ctx, len, requests, scale, causal, window, most, y.p, y.ld,
-                                       ws, bytes, st);
+            return cache_lib.paged_attention(q.p, q.ld, q.rows, q.heads, cache, &f.f, t.p, t.ld, t.columns, cu, ctx, len, requests, scale, causal, window,
+                                             most, y.p, y.ld, ws, bytes, st);
         };
     });
 }
@@ -463,10 +466,12 @@ PyObject *bind_format(PyObject *, PyObject *type)
     Py_RETURN_NONE;
 }
 
-// bind(addresses): the entry points of the library that binding.py has loaded, in the order of struct Library
-PyObject *bind(PyObject *, PyObject *addresses)
+// bind(addresses), bind_cache(addresses): the entry points of the library that binding.py has loaded, in the order of struct Library and of
+// struct CacheLibrary
+template <typename LIBRARY>
+PyObject *bind_to(LIBRARY &to, PyObject *addresses)
 {
-    constexpr Py_ssize_t COUNT = sizeof(Library) / sizeof(void *);
+    constexpr Py_ssize_t COUNT = sizeof(LIBRARY) / sizeof(void *);
     if (!PyTuple_CheckExact(addresses) || PyTuple_GET_SIZE(addresses) != COUNT) {
         PyErr_SetString(PyExc_TypeError, "bind takes a tuple of addresses");
         return nullptr;
@@ -476,15 +481,19 @@ PyObject *bind(PyObject *, PyObject *addresses)
         p[i] = PyLong_AsVoidPtr(PyTuple_GET_ITEM(addresses, i));
         if (PyErr_Occurred()) return nullptr;
     }
-    static_assert(sizeof(lib) == sizeof(p), "pointers only");
-    memcpy(&lib, p, sizeof(lib));
+    static_assert(sizeof(to) == sizeof(p), "pointers only");
+    memcpy(&to, p, sizeof(to));
     Py_RETURN_NONE;
 }
+PyObject *bind(PyObject *, PyObject *addresses) { return bind_to(lib, addresses); }
+PyObject *bind_cache(PyObject *, PyObject *addresses) { return bind_to(cache_lib, addresses); }
 
 #define QL_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {QL_METHOD(w8a8_linear), QL_METHOD(w4a8_linear), QL_METHOD(w8a8_gemm), QL_METHOD(w4a8_gemm), QL_METHOD(quant_act),
-                         QL_METHOD(quant_rmsnorm), QL_METHOD(quant_swiglu), QL_METHOD(quant_transformed), QL_METHOD(kv_resize), QL_METHOD(kv_append), QL_METHOD(kv_read),
-                         QL_METHOD(paged_attention), {"bind_format", bind_format, METH_O, nullptr}, {"bind", bind, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         QL_METHOD(quant_rmsnorm), QL_METHOD(quant_swiglu), QL_METHOD(quant_transformed),
+                         QL_METHOD(kv_resize), QL_METHOD(kv_append), QL_METHOD(kv_read), QL_METHOD(paged_attention),
+                         {"bind", bind, METH_O, nullptr}, {"bind_cache", bind_cache, METH_O, nullptr},
+                         {"bind_format", bind_format, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_qlcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
