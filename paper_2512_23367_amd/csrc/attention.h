@@ -99,9 +99,9 @@ __device__ inline int wave_most(int v) { return wave_all(v, [](int a, int b) { r
 // Decode steps, 8 heads, int8, cut into work / slots units for 512 and for 256 workgroups (a few CUs get one more than the others): four
 // requests of 60000..131072 tokens 184, 193 us, this way 157; 32 requests of 200..4096 tokens 40, 37 us, this way 35; four new tokens
 // each (32 rows) on four requests of 30000..60000: one workgroup a CU 139 us, two 114.
-// Tiles of 128 rows wait for themselves rather than for memory -- a unit takes a workgroup alone on its CU 1.3 us at D = 64, 1.9 at 128, 3.7
-// at 256 --, and their partial results weigh more: they are cut where that is faster by these times.  Over 120 mixed prompts and chunks 0.8 %
-// slower than the better of cutting and not cutting for each, always cutting 1.4 %, never 27 %.
+// Tiles of 128 rows wait for themselves rather than for memory, and their partial results weigh more: they are cut where that is faster by
+// times fitted to parts (a unit 1.3 us at D = 64, 1.9 at 128, 3.7 at 256, with what writing the part costs).  Over 120 mixed prompts and chunks 0.8 %
+// slower than the better of cutting and not cutting for each, always cutting 1.4 %, never 26 %.
 template <int bm, typename COUNT>
 __device__ inline float attn_part_units(const KvView &kv, float tiles, float work, float most, int slots, COUNT parts_of_all)
 {
