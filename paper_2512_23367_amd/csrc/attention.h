@@ -304,7 +304,7 @@ __host__ __device__ inline size_t attn_notes_bytes(int tiles) { return ((size_t)
 
 struct AttnPlan {
     int bm;              // rows of a tile
-    int step;            // 1: the kernel for few rows, whose wavefronts share a tile's tokens
+    int step;            // 1: the kernel for few rows, whose wavefronts share a tile's tokens; 2: requests are short
     int slots;           // see attn_part_units (0: a workgroup per tile, no parts)
     int tiles, items;    // tiles of a key/value head, at most, and workgroups
     int far_first;       // whole tiles in the order of what they see, over all requests: at most eight workgroups for every CU

@@ -117,7 +117,7 @@ int launch_attention(const AttnArgs &a, hipStream_t st)
         if (!a.ws) return fail(QL_ERR_NULL, "ws is NULL");
         if (a.ws_bytes < p.ws_bytes) return fail(QL_ERR_WORKSPACE, "workspace has %zu bytes, this call needs %zu (see ql_paged_attention_bytes)", a.ws_bytes, p.ws_bytes);
     }
-    if ((int64_t)a.columns << a.kv.page_shift <= (p.step ? SHORT : SHORT / 2)) p.slots = 0, p.items = p.tiles, p.far_first = !p.step;
+    if ((int64_t)a.columns << a.kv.page_shift <= (p.step ? SHORT : SHORT / 2)) p.slots = 0, p.items = p.tiles, p.far_first = !p.step, p.step *= 2;
     if ((int64_t)p.items * a.kv.heads >= (int64_t)1 << 31)
         return fail(QL_ERR_UNSUPPORTED, "%d tokens of %d query heads are more than a launch holds", a.T, a.q_heads);
     // exp(scale s) = exp2(c s); a scale of nothing keeps masked scores apart from the others (-inf times 0 would be NaN)

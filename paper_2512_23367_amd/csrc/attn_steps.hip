@@ -26,8 +26,9 @@ __device__ inline float over_quarters(float v, OP op)                // of the l
     return op(__builtin_bit_cast(float, x), __builtin_bit_cast(float, y));
 }
 
-template <int ELEM, int D, int NQ>
-__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attn_step_kernel(AttnArgs a, AttnPlan plan, float c, unsigned flip)
+// OCC: workgroups of a CU at least
+template <int ELEM, int D, int NQ, int OCC>
+__global__ __launch_bounds__(256, OCC) void attn_step_kernel(AttnArgs a, AttnPlan plan, float c, unsigned flip)
 {
     constexpr int BM = 16 * NQ, NW = 4;
     constexpr int TOK = ELEM == 2 ? 32 : 64;                         // tokens of a wavefront's turn: 64 bytes of every lane's keys and values at D = 128
@@ -329,11 +330,15 @@ int launch(const AttnArgs &a, const AttnPlan &p, float c, unsigned flip, hipStre
     const unsigned grid = (unsigned)(p.items * a.kv.heads);
     if constexpr (D < 256) {
         if (p.bm == 32) {
-            attn_step_kernel<ELEM, D, 2><<<grid, 256, 0, st>>>(a, p, c, flip);
+            attn_step_kernel<ELEM, D, 2, 2><<<grid, 256, 0, st>>>(a, p, c, flip);
             return check_hip(hipGetLastError(), "attn_step_kernel");
         }
     }
-    attn_step_kernel<ELEM, D, 1><<<grid, 256, 0, st>>>(a, p, c, flip);
+    // D = 256: one workgroup a CU with registers for all, but two where requests are short and their workgroups wait more than they load; int8
+    // spills (us, one / two; 8 heads, 126 requests of 40, 250 and 900 tokens: fp16 38.5 / 23.6, 68.5 / 59.0, 170 / 171, 32 of 200..4096 114 / 124; int8
+    // 40 / 27, 54 / 54, 109 / 145).
+    if (D < 256 || (ELEM == 2 && p.step == 2)) attn_step_kernel<ELEM, D, 1, ELEM == 1 && D == 256 ? 1 : 2><<<grid, 256, 0, st>>>(a, p, c, flip);
+    else attn_step_kernel<ELEM, D, 1, D == 256 ? 1 : 2><<<grid, 256, 0, st>>>(a, p, c, flip);
     return check_hip(hipGetLastError(), "attn_step_kernel");
 }
 
