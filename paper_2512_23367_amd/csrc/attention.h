@@ -25,6 +25,11 @@ typedef unsigned u4 __attribute__((ext_vector_type(4)));
 constexpr int ATTN_UNIT = 64;            // tokens that tiles of keys are aligned to, and parts of a row's tokens
 constexpr int ATTN_THREADS = 512;
 
+// Weights are 2^(score - maximum + ATTN_LEAD): fp16 reaches 2^16, the maximum that the kernels keep may be 2^8 behind, and what is left goes to the
+// small ones.  Rounded to fp16 they lose 2^-11 of themselves down to 2^-21 of the maximum's weight, below it 2^-32 of that (without the lead 2^-25: of
+// 120000 tokens of 2^-25 each behind one far ahead nothing was left, 0.3 % of the sum).
+constexpr float ATTN_LEAD = 7.0f;
+
 // r / group: see AttnArgs::group_mul
 __device__ inline int attn_token(const AttnArgs &a, int r) { return (int)((__umulhi((unsigned)r, a.group_mul) + (unsigned)r) >> a.group_shift); }
 

@@ -230,7 +230,7 @@ __global__ __launch_bounds__(256, OCC) void attn_step_kernel(AttnArgs a, AttnPla
 #pragma unroll
                 for (int j = 0; j < 4; ++j) top = fmaxf(top, s[n][x][j]);
             top = over_quarters(top, [](float x, float y) { return fmaxf(x, y); });
-            // The maximum follows only when a score exceeds it by 2^8: weights up to 256 lose nothing in fp16, and the sums are rarely rescaled.
+            // The maximum follows only when a score exceeds it by 2^8: with ATTN_LEAD weights up to 2^15, and the sums are rarely rescaled.
             if (__any((top - m[n]) * factor > 8.0f)) {
                 const float to = fmaxf(m[n], top), keep = m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[n] - to) * factor);
                 m[n] = to;
@@ -238,18 +238,20 @@ __global__ __launch_bounds__(256, OCC) void attn_step_kernel(AttnArgs a, AttnPla
 #pragma unroll
                 for (int e = 0; e < ET; ++e) o[n][e] *= keep;
             }
-            const float base = m[n] == -INFINITY ? 0.f : -m[n] * factor;
+            const float base = m[n] == -INFINITY ? 0.f : fmaf(-m[n], factor, ATTN_LEAD);
             unsigned w[ST * 2];
+            float sum = 0;                                           // of the turn: a small weight is not lost beside all before it
 #pragma unroll
             for (int x = 0; x < ST; ++x) {
                 float e[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     e[j] = __builtin_amdgcn_exp2f(RAW ? fmaf(s[n][x][j], c, base) : s[n][x][j] + base);
-                    l[n] = ELEM == 1 ? fmaf(e[j], iv[ELEM == 1 ? 4 * x + j : 0], l[n]) : l[n] + e[j];
+                    sum = ELEM == 1 ? fmaf(e[j], iv[ELEM == 1 ? 4 * x + j : 0], sum) : sum + e[j];
                 }
                 w[2 * x] = pack2(e[0], e[1]), w[2 * x + 1] = pack2(e[2], e[3]);
             }
+            l[n] += sum;
             p[n][0] = as_h8(u4{w[0], w[1], w[2], w[3]});
             if constexpr (ELEM == 1) p[n][1] = as_h8(u4{w[4], w[5], w[6], w[7]});
         }

@@ -93,3 +93,63 @@ def test_many_requests_without_parts(U, D, requests, new_most, max_new, bits):
 def test_every_token_sees_every_token_of_wider_heads(U, ctx, new, heads, kv_heads, D, bits):
     r = U.Requests(D, ctx, new, heads, kv_heads, D, bits, 32)
     r.check(r.call(causal=False), causal=False)
+
+
+def _tail(U, bits, D, kv_heads, t, v_tail, n):
+    """A cache of two pages of 1024 tokens, key (score in powers of two, 0, 0, ...): a first token of score 0 and value 1, all others of score -t
+    and value v_tail; block table entries for n tokens."""
+    fmt = ql.QlKvFormat(heads=kv_heads, head_dim=D, page_size=1024, pages=2, bits=bits)
+    cache = torch.full((ql.ql_kv_cache_bytes(fmt),), 0xFF, dtype=torch.uint8, device=U.DEV)
+    k = torch.zeros((2048, kv_heads, D), dtype=torch.float16, device=U.DEV)
+    v = torch.full_like(k, v_tail)
+    k[1:, :, 0], v[0] = -t, 1.0
+    ql.ql_kv_append(None, k.view(2048, -1), v.view(2048, -1), None, None, U.ints(np.arange(2048)), None, cache, fmt)
+    return fmt, cache, [0] + [1] * (n // 1024 - 1)
+
+
+def _check_tail(y, t, v_tail, n, adds):
+    """y = (1 + tail v_tail) / (1 + tail), tail = (n - 1) 2^-t; sum p |v| / sum p = 1.  Off by: y rounded to fp16, 2^-11 |y|; the weights rounded to fp16, 2^-11 in
+    all (the first one is a power of two); weights below fp16's normal range, which the largest one is 2^7 of at least: 2^-32 each in the sum of the
+    values and in that of the weights; `adds` additions to a sum, each within a step of 2^-23; scores: 2^-22 (|score| + 4), 32 2^-23 for the logarithm of the scale, twice."""
+    tail = (n - 1) * 2.0 ** -t
+    ref = (1 + tail * v_tail) / (1 + tail)
+    tol = 2.0 ** -11 * abs(ref) + 2.0 ** -11 + 2 * n * 2.0 ** -32 + adds * 2.0 ** -23 + 2 * (2.0 ** -22 * (t + 4) + 32 * 2.0 ** -23) + 2.0 ** -24
+    err = (y.double() - ref).abs().max().item()
+    assert err <= tol, f"{err:.3g}, tolerance {tol:.3g}"
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("t", [16, 20.5, 23.25, 24.9375, 25.0625, 27, 30])
+@pytest.mark.parametrize("v_tail", [1.0, -1.0])
+def test_a_long_tail_of_small_weights_few_rows(U, v_tail, t, D, bits):
+    """One token ahead of 2^19 others, none cut into parts: the wavefront that holds the first one adds up a quarter of the others beside it, 32 at a time."""
+    n, requests = 1 << 19, 4200
+    fmt, cache, entries = _tail(U, bits, D, 1, t, v_tail, n)
+    table = torch.zeros((requests, len(entries)), dtype=torch.int32, device=U.DEV)
+    table[7] = U.ints(entries)
+    length = torch.ones(requests, dtype=torch.int32, device=U.DEV)
+    length[7] = n
+    q = torch.zeros((requests, D), dtype=torch.float16, device=U.DEV)
+    q[:, 0] = 1
+    y = torch.zeros_like(q)
+    ws = torch.empty(max(1, ql.ql_paged_attention_bytes(fmt, requests, requests, 1, 1)), dtype=torch.uint8, device=U.DEV)
+    ql.ql_paged_attention(q, cache, fmt, table, U.ints(np.arange(requests + 1)), None, length, float(np.log(2)), y, ws, causal=False, max_new=1)
+    _check_tail(y[7], t, v_tail, n, n / 4 / 32)
+    assert (y[:7] == 1).all() and (y[8:] == 1).all()
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("t", [16, 20.5, 23.25, 24.9375, 25.0625, 27, 30])
+@pytest.mark.parametrize("v_tail", [1.0, -1.0])
+def test_a_long_tail_of_small_weights_many_rows(U, v_tail, t, D, bits):
+    """The same in tiles of 128 (D = 128: 256) rows, too many of them for parts: 120832 tokens, 16 at a time."""
+    n, T, heads, kv_heads = 118 * 1024, 1100, 64, 4
+    fmt, cache, entries = _tail(U, bits, D, kv_heads, t, v_tail, n)
+    q = torch.zeros((T, heads, D), dtype=torch.float16, device=U.DEV)
+    q[..., 0] = 1
+    y = torch.zeros((T, heads * D), dtype=torch.float16, device=U.DEV)
+    ql.ql_paged_attention(q.view(T, -1), cache, fmt, U.ints([entries]), U.ints([0, T]), None, U.ints([n]), float(np.log(2)), y,
+                          torch.empty(max(1, ql.ql_paged_attention_bytes(fmt, T, 1, heads)), dtype=torch.uint8, device=U.DEV), causal=False)
+    _check_tail(y, t, v_tail, n, n / 16)
