@@ -371,7 +371,8 @@ int ql_kv_read(const void *cache, const ql_kv_format *format /* host */, const i
 /* Attention of the requests' new tokens over the cache:
  *   y[t, h] = sum_j p_j v[j, g] / sum_j p_j,   p_j = exp(scale * q[t, h] . k[j, g]),   g = h / (q_heads / heads)
  * over the tokens j of t's request that t sees: all j < kv_len; with `causal` those with j <= position of t as well, and with window > 0
- * position - window < j.  Tokens on pages outside [0, pages) are not seen.  A row that sees nothing is 0.
+ * position - window < j.  Tokens on pages outside [0, pages) are not seen.  A row that sees nothing is 0;
+ * one that sees a token is NaN where its query is infinite or NaN.
  * Scores, maxima, sums and the output are kept in fp32; the p_j are rounded to fp16 for the products with v (those below 2^-21 of the row's
  * largest to multiples of 2^-31 of it or less), the int8 codes take part as they are (their scales in fp32).
  *   q            fp16 [T, q_heads * D], y  fp16 [T, q_heads * D]; y may be q itself (same leading dimension), may otherwise not overlap it

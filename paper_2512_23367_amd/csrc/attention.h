@@ -33,6 +33,14 @@ constexpr float ATTN_LEAD = 7.0f;
 // r / group: see AttnArgs::group_mul
 __device__ inline int attn_token(const AttnArgs &a, int r) { return (int)((__umulhi((unsigned)r, a.group_mul) + (unsigned)r) >> a.group_shift); }
 
+// Eight channels of a query: an infinity becomes NaN (inf * 0), all else stays.  An infinite channel makes every score of its row infinite or NaN, and the
+// softmax of those NaN; by the running maximum alone a row whose scores are all -inf would come out as one that sees nothing.
+__device__ inline h8 attn_query(u4 v)
+{
+    const h8 x = __builtin_bit_cast(h8, v), zero = {};
+    return __builtin_elementwise_fma(x, zero, x);
+}
+
 struct AttnSpan {                        // a request as the kernels see it
     int cu, rows, ctx, len;              // first row of q, rows (new tokens x heads of the group), position of the first new token, tokens
     int low, high;                       // tokens that any of its rows sees; low is a multiple of ATTN_UNIT

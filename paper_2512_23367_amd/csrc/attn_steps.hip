@@ -69,7 +69,7 @@ __global__ __launch_bounds__(256, OCC) void attn_step_kernel(AttnArgs a, AttnPla
             const int d = ELEM == 2 ? 32 * k + 8 * qd : 64 * (k / 2) + 16 * qd + 8 * (k % 2);
             u4 v = {0, 0, 0, 0};
             if (live) v = *reinterpret_cast<const u4 *>(src + d);
-            q[n][k] = as_h8(v ^ flip);
+            q[n][k] = attn_query(v ^ flip);
         }
     }
 

@@ -63,7 +63,7 @@ __global__ __launch_bounds__(NW * 64, D == 256 ? 1 : 2) void attn_tile_kernel(At
             const int d = ELEM == 2 ? 16 * s + 8 * h : 32 * (s / 2) + 16 * h + 8 * (s % 2);
             u4 v = {0, 0, 0, 0};
             if (live) v = *reinterpret_cast<const u4 *>(src + d);
-            q[s] = as_h8(v ^ flip);
+            q[s] = attn_query(v ^ flip);
         }
     }
 

@@ -95,6 +95,39 @@ def test_every_token_sees_every_token_of_wider_heads(U, ctx, new, heads, kv_head
     r.check(r.call(causal=False), causal=False)
 
 
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("new", [[1, 1], [60, 140]])
+def test_queries_that_are_not_finite(U, new, D, bits):
+    """One of them makes every score of its row infinite or NaN, so its row is NaN, with whatever number of tokens it sees (exp(-inf) / 0 where all of its
+    scores are -inf); a row that sees nothing is 0 still.  Nobody else is touched."""
+    r = U.Requests(D, [0, 77], new, 4, 2, D, bits, 32)
+    clean = r.call()
+    r.check(clean)
+    empty = U.Requests(D, [0, 0], new, 4, 2, D, bits, 32, kv_len=[0, 0])
+    for what in (float("inf"), float("-inf"), float("nan")):
+        for t in {0, r.T - 1, new[0]}:
+            for head in (0, 3):
+                for channel in (0, D // 2 + 9, D - 1):
+                    q = U.dev(r.q)
+                    q[t, head * D + channel] = what
+                    y = r.call(q=q).view(r.T, 4, D)
+                    assert torch.isnan(y[t, head]).all(), (what, t, head, channel)
+                    y[t, head] = clean.view(r.T, 4, D)[t, head]
+                    r.check(y, rows=[t, max(0, t - 1), min(r.T - 1, t + 1)])
+                    assert (empty.call(q=q) == 0).all()
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("new", [[1, 1], [60, 140]])
+def test_queries_below_the_normal_range_of_fp16(U, new, D, bits):
+    r = U.Requests(D + 1, [9, 77], new, 4, 2, D, bits, 32)
+    r.q = (r.q.astype(np.float32) * 2.0 ** -18).astype(np.float16)
+    scale = 2.0 ** 18 * D ** -0.5
+    r.check(r.call(scale=scale), scale=scale)
+
+
 def _tail(U, bits, D, kv_heads, t, v_tail, n):
     """A cache of two pages of 1024 tokens, key (score in powers of two, 0, 0, ...): a first token of score 0 and value 1, all others of score -t
     and value v_tail; block table entries for n tokens."""
