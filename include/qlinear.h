@@ -331,18 +331,20 @@ int ql_kv_cache_bytes(const ql_kv_format *format /* host */, size_t *bytes /* ho
  * gives its last pages back, behind the ring's end: pages given back in a call are not taken in the same one.
  *   old_len, want_len  int32 [requests] (negative: 0; old_len beyond columns * page_size counts as that)
  *   ring               int32 [pages]: the free pages, pool[1] of them from place pool[0] on, modulo pages
- *   pool, pool_out     int32 [4]: {first place, number of free pages, tokens left without a slot, 0}; pool_out may be pool.
+ *   pool, pool_out     int32 [4]: {first place, number of free pages, tokens left without a slot, 0}; pool_out may be pool.  Tokens left without
+ *                      a slot: the sum of want_len - kv_len over the requests that do not shrink.
  *                      pool_out[3] has to hold 0 on entry (every call leaves it so).  At the start: {0, pages, 0, 0}, ring 0, 1, 2, ...
  *   block_table        int32 [requests][ld_table], columns used: page of tokens c * page_size ... at [b][c]; entries of pages that the
  *                      call takes are written, all others left as they were
- *   kv_len             int32 [requests]: tokens that have a page now: want_len, less where the ring or the columns did not suffice (the
- *                      next call's old_len)
- *   cu_new             int32 [requests + 1]: new tokens (want - old where that is positive) of the requests before b; at most max_tokens
+ *   kv_len             int32 [requests]: tokens that have a page now: want_len, less where the ring, the columns or max_tokens did not
+ *                      suffice (the next call's old_len)
+ *   cu_new             int32 [requests + 1]: new tokens (want - old where that is positive) of the requests before b; at most max_tokens:
+ *                      those beyond it have no row, and neither page nor slot
  *   slots, positions   int32 [max_tokens], by new token: its slot (-1: no page, the cache is not written and not read for it) and
  *                      its position in the request; entries behind cu_new[requests] are left as they were
  * kv_len, cu_new, slots and positions may not overlap old_len or want_len.
  * Limits: requests <= 4096, requests * columns and columns * page_size < 2^31 (QL_ERR_UNSUPPORTED).  Calls that share a pool, ring or table have to follow
- * each other; requests == 0: cu_new[0] = 0, pool_out = pool. */
+ * each other; requests == 0: cu_new[0] = 0, pool_out = {pool[0], pool[1], 0, 0}. */
 int ql_kv_resize(const int32_t *old_len, const int32_t *want_len, int requests, int page_size, int32_t *ring, int pages,
                  const int32_t *pool, int32_t *pool_out, int32_t *block_table, int64_t ld_table, int columns, int32_t *kv_len,
                  int32_t *cu_new, int32_t *slots, int32_t *positions, int max_tokens, void *stream);

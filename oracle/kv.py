@@ -42,7 +42,7 @@ def resize(old, want, page, ring, pool, table, max_tokens):
             p = o + i
             positions.append(p)
             slots.append(table[b][p // page] * page + p % page if p < length else -1)
-        lost += o + n - length
+        lost += w - length                            # for want of a page, a column or a row
         kv_len.append(length)
         cu.append(cu[-1] + n)
     pool_out = [(head + taken) % n_pages, free - taken + given, lost, 0]

@@ -125,7 +125,7 @@ __global__ __launch_bounds__(RESIZE_THREADS) void kv_resize_kernel(ResizeArgs a)
         const int len = w < o ? w : (int)min((int64_t)t, (int64_t)(has + got) << a.page_shift);
         if (b <= B) cu[b] = from, takes[b] = taken, gives[b] = (int)(before.pages >> 32);
         if (b < B) {
-            if (w >= o) lost += (int64_t)o + n - len;
+            if (w >= o) lost += (int64_t)w - len;              // (for want of a page, a column of the table or a row of the step)
             if (blockIdx.x == 0) a.kv_len[b] = len, a.cu_new[b] = from;
         }
         before.tokens += max(0, w - o), before.pages += moved(o, t);

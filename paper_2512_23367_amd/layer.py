@@ -97,7 +97,7 @@ class PagedRequests:
         self.fmt, self.max_requests, self.max_tokens = fmt, max_requests, max_tokens
         self.block_table = ints(max_requests, columns)
         self.ring = torch.arange(fmt.pages, dtype=torch.int32, device=device)
-        self.pool = torch.tensor([0, fmt.pages, 0, 0], dtype=torch.int32, device=device)   # [2]: tokens that found no page
+        self.pool = torch.tensor([0, fmt.pages, 0, 0], dtype=torch.int32, device=device)   # [2]: tokens that found no page or row
         self.ctx_len, self.kv_len, self.cu_new = ints(max_requests), ints(max_requests), ints(max_requests + 1)
         self.slots, self.positions = ints(max_tokens), ints(max_tokens)
         self.max_new = 0
