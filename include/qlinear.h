@@ -386,7 +386,7 @@ int ql_kv_read(const void *cache, const ql_kv_format *format /* host */, const i
  *                kernel, never into the result's correctness
  *   ws           workspace, 256-byte aligned: partial results of requests whose tokens several workgroups share.  One call at a time;
  *                nothing in it is kept.  ql_paged_attention_bytes: enough for these sizes and smaller ones -- fewer tokens or requests, a
- *                smaller max_new (0, not known, is the largest); at most 136 MB
+ *                smaller max_new (0, not known, is the largest); at most 137 MB
  * q_heads is a multiple of heads; window >= 0, and 0 without causal; scale finite.  At most 65536 requests, T * q_heads / heads < 2^28. */
 int ql_paged_attention_bytes(const ql_kv_format *format /* host */, int T, int requests, int q_heads, int max_new, size_t *bytes /* host */);
 int ql_paged_attention(const void *q, int64_t ldq, int T, int q_heads, const void *cache, const ql_kv_format *format /* host */,
