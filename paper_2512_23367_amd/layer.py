@@ -119,7 +119,7 @@ class PagedDecoderLayer(DecoderLayerLinears):
     def __init__(self, w_qkv, w_o, w_gate_up, w_down, bits: int, max_tokens: int, fmt: ql.QlKvFormat, cos_sin, max_requests: int,
                  biases=None, scale=None):
         """w_qkv fp16 [(q_heads + 2 heads) head_dim, d], w_o [d, q_heads head_dim], the others as in DecoderLayerLinears; cos_sin:
-        rotary table of ql_kv_append; scale: of the scores, head_dim ** -0.5 by default."""
+        rotary table of ql_kv_append (None: a layer without rotary embedding); scale: of the scores, head_dim ** -0.5 by default."""
         self.fmt, self.cos_sin = fmt, cos_sin
         self.q_heads = w_o.shape[1] // fmt.head_dim
         self.scale = fmt.head_dim ** -0.5 if scale is None else scale
@@ -144,7 +144,8 @@ class PagedDecoderLayer(DecoderLayerLinears):
         self._linear(x, "qkv", y_qkv)
         nq, nk = self.q_heads * D, self.fmt.heads * D
         q, k, v = y_qkv[:, :nq], y_qkv[:, nq:nq + nk], y_qkv[:, nq + nk:]
-        ql.ql_kv_append(q, k, v, self.cos_sin, requests.positions[:M], requests.slots[:M], q, cache, self.fmt)
+        turned = q if self.cos_sin is not None else None                 # (ql_kv_append takes queries only to turn them)
+        ql.ql_kv_append(turned, k, v, self.cos_sin, requests.positions[:M], requests.slots[:M], turned, cache, self.fmt)
         ql.ql_paged_attention(q, cache, self.fmt, requests.block_table, requests.cu_new, requests.ctx_len, requests.kv_len, self.scale, y_attention,
                               self.attention_ws, max_new=requests.max_new)
         return self._behind_attention(y_attention)
