@@ -163,11 +163,12 @@ const int8_t *codes(PyObject *o, int M, int K)
     return static_cast<const int8_t *>(t.data_ptr());
 }
 
-// The call itself, without the interpreter's lock (as ctypes makes it); None if an argument was not plain.
+// The call itself, without the interpreter's lock (as ctypes makes it); None if an argument was not plain or the functions are not bound (`bound`: the address
+// of one of them).
 template <typename Prepare>
-PyObject *call(Py_ssize_t given, Py_ssize_t wanted, Prepare prepare)
+PyObject *call(Py_ssize_t given, Py_ssize_t wanted, bool bound, Prepare prepare)
 {
-    if (given != wanted || !lib.weight_bytes) Py_RETURN_NONE;
+    if (given != wanted || !bound) Py_RETURN_NONE;
     int status;
     try {
         auto launch = prepare();
@@ -187,7 +188,7 @@ using Args = PyObject *const *;
 
 PyObject *w8a8_linear(PyObject *, Args a, Py_ssize_t n)   // x, wq_kernel, sw, bias, N, y, ws, stream
 {
-    return call(n, 8, [&] {
+    return call(n, 8, lib.weight_bytes, [&] {
         const Matrix x(a[0]);
         const int N = as_int(a[4]);
         const void *w = blob(a[1], N, x.columns, 8, 0), *b = bias_of(a[3], N);
@@ -201,7 +202,7 @@ PyObject *w8a8_linear(PyObject *, Args a, Py_ssize_t n)   // x, wq_kernel, sw, b
 
 PyObject *w4a8_linear(PyObject *, Args a, Py_ssize_t n)   // x, w4_kernel, group, bias, N, y, ws, stream
 {
-    return call(n, 8, [&] {
+    return call(n, 8, lib.weight_bytes, [&] {
         const Matrix x(a[0]);
         const int group = as_int(a[2]), N = as_int(a[4]);
         const void *w = blob(a[1], N, x.columns, 4, group), *b = bias_of(a[3], N);
@@ -214,7 +215,7 @@ PyObject *w4a8_linear(PyObject *, Args a, Py_ssize_t n)   // x, w4_kernel, group
 
 PyObject *w8a8_gemm(PyObject *, Args a, Py_ssize_t n)   // xq_kernel, sx, M, K, wq_kernel, sw, bias, N, y, ws, stream
 {
-    return call(n, 11, [&] {
+    return call(n, 11, lib.weight_bytes, [&] {
         const int M = as_int(a[2]), K = as_int(a[3]), N = as_int(a[7]);
         const int8_t *xq = codes(a[0], M, K);
         const float *sx = floats(a[1], M), *sw = floats(a[5], N);
@@ -228,7 +229,7 @@ PyObject *w8a8_gemm(PyObject *, Args a, Py_ssize_t n)   // xq_kernel, sx, M, K, 
 
 PyObject *w4a8_gemm(PyObject *, Args a, Py_ssize_t n)   // xq_kernel, sx, M, K, w4_kernel, group, bias, N, y, ws, stream
 {
-    return call(n, 11, [&] {
+    return call(n, 11, lib.weight_bytes, [&] {
         const int M = as_int(a[2]), K = as_int(a[3]), group = as_int(a[5]), N = as_int(a[7]);
         const int8_t *xq = codes(a[0], M, K);
         const float *sx = floats(a[1], M);
@@ -242,7 +243,7 @@ PyObject *w4a8_gemm(PyObject *, Args a, Py_ssize_t n)   // xq_kernel, sx, M, K, 
 
 PyObject *quant_act(PyObject *, Args a, Py_ssize_t n)   // x, xq_rowmajor, xq_kernel, sx, stream
 {
-    return call(n, 5, [&] {
+    return call(n, 5, lib.weight_bytes, [&] {
         const Matrix x(a[0]);
         int8_t *rm = pointer<int8_t>(a[1]), *kl = pointer<int8_t>(a[2]);
         float *sx = pointer<float>(a[3]);
@@ -253,7 +254,7 @@ PyObject *quant_act(PyObject *, Args a, Py_ssize_t n)   // x, xq_rowmajor, xq_ke
 
 PyObject *quant_rmsnorm(PyObject *, Args a, Py_ssize_t n)   // x, gamma, eps, xq_rowmajor, xq_kernel, sx, stream
 {
-    return call(n, 7, [&] {
+    return call(n, 7, lib.weight_bytes, [&] {
         const Matrix x(a[0]);
         const void *gamma = tensor(a[1], at::kHalf).data_ptr();
         const float eps = as_float(a[2]);
@@ -266,7 +267,7 @@ PyObject *quant_rmsnorm(PyObject *, Args a, Py_ssize_t n)   // x, gamma, eps, xq
 
 PyObject *quant_swiglu(PyObject *, Args a, Py_ssize_t n)   // gate_up, xq_rowmajor, xq_kernel, sx, stream
 {
-    return call(n, 5, [&] {
+    return call(n, 5, lib.weight_bytes, [&] {
         const Matrix x(a[0]);
         if (x.columns % 2) throw NotPlain();
         int8_t *rm = pointer<int8_t>(a[1]), *kl = pointer<int8_t>(a[2]);
@@ -278,7 +279,7 @@ PyObject *quant_swiglu(PyObject *, Args a, Py_ssize_t n)   // gate_up, xq_rowmaj
 
 PyObject *quant_transformed(PyObject *, Args a, Py_ssize_t n)   // x, inv_smooth, hadamard_block, xq_rowmajor, xq_kernel, sx, stream
 {
-    return call(n, 7, [&] {
+    return call(n, 7, lib.weight_bytes, [&] {
         const Matrix x(a[0]);
         const float *inv = pointer<float>(a[1]);
         const int block = as_int(a[2]);
@@ -371,7 +372,7 @@ int as_flag(PyObject *o)
 // page_size, old_len, want_len, ring, pool, pool_out, block_table, kv_len, cu_new, slots, positions, stream
 PyObject *kv_resize(PyObject *, Args a, Py_ssize_t n)
 {
-    return call(n, 12, [&] {
+    return call(n, 12, cache_lib.kv_cache_bytes, [&] {
         const Here here;
         const int page = as_int(a[0]), requests = as_int(here(a[1]).numel()), pages = as_int(here(a[3]).numel());
         const int most = as_int(std::min(here(a[9]).numel(), here(a[10]).numel()));
@@ -388,7 +389,7 @@ PyObject *kv_resize(PyObject *, Args a, Py_ssize_t n)
 
 PyObject *kv_append(PyObject *, Args a, Py_ssize_t n)   // q, k, v, cos_sin, positions, slots, q_out, cache, fmt, stream
 {
-    return call(n, 10, [&] {
+    return call(n, 10, cache_lib.kv_cache_bytes, [&] {
         const Here here;
         const Format f(a[8]);
         const Rows k(here, a[1], f.f.head_dim), v(here, a[2], f.f.head_dim);
@@ -418,7 +419,7 @@ PyObject *kv_append(PyObject *, Args a, Py_ssize_t n)   // q, k, v, cos_sin, pos
 
 PyObject *kv_read(PyObject *, Args a, Py_ssize_t n)   // cache, fmt, slots, k, v, stream
 {
-    return call(n, 6, [&] {
+    return call(n, 6, cache_lib.kv_cache_bytes, [&] {
         const Here here;
         const Format f(a[1]);
         Rows k, v;
@@ -437,7 +438,7 @@ PyObject *kv_read(PyObject *, Args a, Py_ssize_t n)   // cache, fmt, slots, k, v
 // q, cache, fmt, block_table, cu_new, ctx_len, kv_len, scale, y, ws, causal, window, max_new, stream
 PyObject *paged_attention(PyObject *, Args a, Py_ssize_t n)
 {
-    return call(n, 14, [&] {
+    return call(n, 14, cache_lib.kv_cache_bytes, [&] {
         const Here here;
         const Format f(a[2]);
         const Rows q(here, a[0], f.f.head_dim), y(here, a[8], f.f.head_dim);
