@@ -382,12 +382,12 @@ int ql_kv_read(const void *cache, const ql_kv_format *format /* host */, const i
  *                the new tokens of request b, which are not decreasing; rows from cu_new[requests] on are left as they were
  *   ctx_len      int32 [requests]: position of a request's first new token (may be NULL without `causal`)
  *   kv_len       int32 [requests]: tokens in the cache, the new ones among them (at most columns * page_size count, which is at most 2^30)
- *   max_new      the most new tokens that a request has, as far as the caller knows it (0: not known): goes into the choice of the
- *                kernel, never into the result's correctness
+ *   max_new      the most new tokens that a request has, as far as the caller knows it (0: not known, taken for T): goes into the choice
+ *                of the kernel, never into the result's correctness
  *   ws           workspace, 256-byte aligned: partial results of requests whose tokens several workgroups share.  One call at a time;
  *                nothing in it is kept.  ql_paged_attention_bytes: enough for these sizes and smaller ones -- fewer tokens or requests, a
  *                smaller max_new (0, not known, is the largest); at most 137 MB
- * q_heads is a multiple of heads; window >= 0, and 0 without causal; scale finite.  At most 65536 requests, T * q_heads / heads < 2^28. */
+ * q_heads is a multiple of heads; window >= 0, and 0 without causal; scale finite, and scale * (q . k) within fp32.  At most 65536 requests, T * q_heads / heads < 2^28. */
 int ql_paged_attention_bytes(const ql_kv_format *format /* host */, int T, int requests, int q_heads, int max_new, size_t *bytes /* host */);
 int ql_paged_attention(const void *q, int64_t ldq, int T, int q_heads, const void *cache, const ql_kv_format *format /* host */,
                        const int32_t *block_table, int64_t ld_table, int columns, const int32_t *cu_new, const int32_t *ctx_len,

@@ -332,12 +332,13 @@ int launch(const AttnArgs &a, const AttnPlan &p, float c, unsigned flip, hipStre
     const unsigned grid = (unsigned)(p.items * a.kv.heads);
     if constexpr (D < 256) {
         if (p.bm == 32) {
+            // (int8, D = 128, spills 15 registers; its reloads in the loop wait for the next turn's keys)
             attn_step_kernel<ELEM, D, 2, 2><<<grid, 256, 0, st>>>(a, p, c, flip);
             return check_hip(hipGetLastError(), "attn_step_kernel");
         }
     }
-    // D = 256: one workgroup a CU with registers for all, but two where requests are short and their workgroups wait more than they load; int8
-    // spills (us, one / two; 8 heads, 126 requests of 40, 250 and 900 tokens: fp16 38.5 / 23.6, 68.5 / 59.0, 170 / 171, 32 of 200..4096 114 / 124; int8
+    // D = 256: one workgroup a CU with registers for all, but two where requests are short and their workgroups wait more than they load (fp16 spills
+    // three registers there, int8 many; us, one / two; 8 heads, 126 requests of 40, 250 and 900 tokens: fp16 38.5 / 23.6, 68.5 / 59.0, 170 / 171, 32 of 200..4096 114 / 124; int8
     // 40 / 27, 54 / 54, 109 / 145).
     if (D < 256 || (ELEM == 2 && p.step == 2)) attn_step_kernel<ELEM, D, 1, ELEM == 1 && D == 256 ? 1 : 2><<<grid, 256, 0, st>>>(a, p, c, flip);
     else attn_step_kernel<ELEM, D, 1, D == 256 ? 1 : 2><<<grid, 256, 0, st>>>(a, p, c, flip);

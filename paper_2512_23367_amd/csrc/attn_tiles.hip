@@ -91,7 +91,8 @@ __global__ __launch_bounds__(NW * 64, D == 256 ? 1 : 2) void attn_tile_kernel(At
     };
     auto block_at = [&](int page, int t) { return a.kv.block(max(page, 0), kvh, t & (a.kv.page_size() - 1)); };
 
-    int pages[DIST + 1][TB];                                         // of the tile at hand, of the next ones
+    // of the tile at hand, of the next ones (int8: in private memory, 32 bytes that every turn stores, as clear() picks them by lane)
+    int pages[DIST + 1][TB];
 
     // ---- a tile into LDS ----
     constexpr int PIECES = ELEM == 2 ? TB * BLOCK / 1024 / NW : TB * BLOCK / 2 / 1024 / NW;   // KB per wavefront, as stored
