@@ -29,15 +29,20 @@ constexpr int ATTN_THREADS = 512;
 // small ones.  Rounded to fp16 they lose 2^-11 of themselves down to 2^-21 of the maximum's weight, below it 2^-32 of that (without the lead 2^-25: of
 // 120000 tokens of 2^-25 each behind one far ahead nothing was left, 0.3 % of the sum).
 constexpr float ATTN_LEAD = 7.0f;
+// Maxima beyond this (in powers of two) are subtracted from the scores before the factor is applied: 2^(fma(s, c, 7 - m c)) takes fewer operations, but what is lost
+// in rounding m c is a factor of all of a row's weights, which takes them out of fp16 from 2^24 on (a row of NaN).  The branch costs 0.5 % (16384 tokens
+// 1996 us, 2001; decode steps 33.9 as without it), small prompts of D = 64 1.5 %.
+constexpr float ATTN_FAR = 1024.0f;
+__device__ inline bool attn_far(float m, float factor) { return m != -INFINITY && __builtin_fabsf(m) * factor > ATTN_FAR; }
 
 // r / group: see AttnArgs::group_mul
 __device__ inline int attn_token(const AttnArgs &a, int r) { return (int)((__umulhi((unsigned)r, a.group_mul) + (unsigned)r) >> a.group_shift); }
 
 // Eight channels of a query: an infinity becomes NaN (inf * 0), all else stays.  An infinite channel makes every score of its row infinite or NaN, and the
 // softmax of those NaN; by the running maximum alone a row whose scores are all -inf would come out as one that sees nothing.
-__device__ inline h8 attn_query(u4 v)
+__device__ inline h8 attn_query(h8 x)
 {
-    const h8 x = __builtin_bit_cast(h8, v), zero = {};
+    const h8 zero = {};
     return __builtin_elementwise_fma(x, zero, x);
 }
 
@@ -306,8 +311,8 @@ __device__ inline void attn_part_range(int &low, int &high, int part, int parts)
     low = (int)min((int64_t)low + (int64_t)part * each, (int64_t)end), high = (int)min((int64_t)low + each, (int64_t)end);
 }
 
-// Workspace: for every tile a note of what there is to join, then for every item and key/value head bm rows of D fp32 sums, bm maxima (in
-// powers of two) and bm sums of the weights.
+// Workspace: for every tile a note of what there is to join, then for every item and key/value head bm rows of D fp32 sums, bm maxima (as the
+// kernels keep them: times `factor`, in powers of two) and bm sums of the weights.
 struct alignas(16) AttnNote {
     int parts, item;                     // of the tile (0 or 1: nothing to join), the first one's number
     int cu, row0, rows, unused[3];       // first row of q, first row of the tile, rows of the request

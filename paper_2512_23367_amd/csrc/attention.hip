@@ -10,7 +10,7 @@ namespace {
 // Joins the parts of the rows whose tokens several workgroups shared: a thread takes 4 channels of a row, eight parts at a time with their
 // weights, all asked for at once.  Bound by latency: the note, then the parts.
 template <int D>
-__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, AttnPlan plan)
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, AttnPlan plan, float factor)
 {
     constexpr int LANES = D / 4, ROWS = 256 / LANES;
     const int kvh = blockIdx.x % a.kv.heads, at = blockIdx.y * ROWS + threadIdx.x / LANES, channel = threadIdx.x % LANES * 4;
@@ -39,11 +39,11 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, AttnPlan pla
             lk[i] = k0 + i < parts ? lk[i] : 0.f;
             top = fmaxf(top, mk[i]);
         }
-        const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+        const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - top) * factor);
         l *= keep, o *= keep, m = top;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float w = lk[i] == 0.f ? 0.f : __builtin_amdgcn_exp2f(mk[i] - top);   // (lk 0: nothing seen, its sums are 0; NaN stays)
+            const float w = lk[i] == 0.f ? 0.f : __builtin_amdgcn_exp2f((mk[i] - top) * factor);   // (lk 0: nothing seen, its sums are 0; NaN stays)
             l += lk[i] * w;
 #pragma unroll
             for (int c = 0; c < 4; ++c) o[c] = fmaf(v[i][c], w, o[c]);
@@ -127,9 +127,10 @@ int launch_attention(const AttnArgs &a, hipStream_t st)
     QL_TRY(p.step ? launch_attention_steps(a, p, c, st) : launch_attention_tiles(a, p, c, st));
     if (!p.slots) return QL_OK;
     const dim3 grid(p.tiles * a.kv.heads, p.bm * a.kv.D / 1024);
-    if (a.kv.D == 64) attn_join_kernel<64><<<grid, 256, 0, st>>>(a, p);
-    else if (a.kv.D == 128) attn_join_kernel<128><<<grid, 256, 0, st>>>(a, p);
-    else attn_join_kernel<256><<<grid, 256, 0, st>>>(a, p);
+    const float factor = a.kv.bits == 16 ? c : 1.0f;                 // (int8: in the scores already, with the keys' scales)
+    if (a.kv.D == 64) attn_join_kernel<64><<<grid, 256, 0, st>>>(a, p, factor);
+    else if (a.kv.D == 128) attn_join_kernel<128><<<grid, 256, 0, st>>>(a, p, factor);
+    else attn_join_kernel<256><<<grid, 256, 0, st>>>(a, p, factor);
     return check_hip(hipGetLastError(), "attn_join_kernel");
 }
 

@@ -69,7 +69,7 @@ __global__ __launch_bounds__(256, OCC) void attn_step_kernel(AttnArgs a, AttnPla
             const int d = ELEM == 2 ? 32 * k + 8 * qd : 64 * (k / 2) + 16 * qd + 8 * (k % 2);
             u4 v = {0, 0, 0, 0};
             if (live) v = *reinterpret_cast<const u4 *>(src + d);
-            q[n][k] = attn_query(v ^ flip);
+            q[n][k] = as_h8(v ^ flip);
         }
     }
 
@@ -126,10 +126,13 @@ __global__ __launch_bounds__(256, OCC) void attn_step_kernel(AttnArgs a, AttnPla
     };
 
     f4 o[NQ][ET];
+    constexpr bool RAW = ELEM == 2;                                  // scores and maxima still without the factor c
+    const float factor = RAW ? c : 1.0f;
     float m[NQ], l[NQ];
+    bool far[NQ];                                                    // of the wavefront: see ATTN_FAR
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
-        m[n] = -INFINITY, l[n] = 0;
+        m[n] = -INFINITY, l[n] = 0, far[n] = false;
 #pragma unroll
         for (int e = 0; e < ET; ++e) o[n][e] = f4{0, 0, 0, 0};
     }
@@ -139,6 +142,10 @@ __global__ __launch_bounds__(256, OCC) void attn_step_kernel(AttnArgs a, AttnPla
         look_up(0);
         load_keys(0);
         load_values(0);
+#pragma unroll
+        for (int n = 0; n < NQ; ++n)
+#pragma unroll
+            for (int k = 0; k < KT; ++k) q[n][k] = attn_query(q[n][k]);   // (behind the loads, which need not wait for them)
     }
     for (int i = 0; i < turns; ++i) {
         const int t = token_of(i);
@@ -210,8 +217,6 @@ __global__ __launch_bounds__(256, OCC) void attn_step_kernel(AttnArgs a, AttnPla
                 for (int e = 0; e < VL; ++e) vx[e] &= clean;
             }
         }
-        constexpr bool RAW = ELEM == 2;                              // scores still without the factor c
-        const float factor = RAW ? c : 1.0f;
         h8 p[NQ][ELEM == 2 ? 1 : 2];
         float iv[ELEM == 1 ? ST * 4 : 1];
         if constexpr (ELEM == 1) {
@@ -234,11 +239,21 @@ __global__ __launch_bounds__(256, OCC) void attn_step_kernel(AttnArgs a, AttnPla
             if (__any((top - m[n]) * factor > 8.0f)) {
                 const float to = fmaxf(m[n], top), keep = m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[n] - to) * factor);
                 m[n] = to;
+                far[n] = __any(attn_far(to, factor));
                 l[n] *= keep;
 #pragma unroll
                 for (int e = 0; e < ET; ++e) o[n][e] *= keep;
             }
-            const float base = m[n] == -INFINITY ? 0.f : fmaf(-m[n], factor, ATTN_LEAD);
+            float base = m[n] == -INFINITY ? 0.f : fmaf(-m[n], factor, ATTN_LEAD);
+            if (far[n]) {
+                asm volatile("");                                    // (a branch: hardly any call takes it)
+                const float off = m[n] == -INFINITY ? 0.f : m[n];
+#pragma unroll
+                for (int x = 0; x < ST; ++x)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s[n][x][j] -= off;
+                base = ATTN_LEAD;
+            }
             unsigned w[ST * 2];
             float sum = 0;                                           // of the turn: a small weight is not lost beside all before it
 #pragma unroll
@@ -277,7 +292,6 @@ __global__ __launch_bounds__(256, OCC) void attn_step_kernel(AttnArgs a, AttnPla
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
         l[n] = over_quarters(l[n], [](float x, float y) { return x + y; });
-        if (ELEM == 2) m[n] *= c;
         if (qd == 0) sm[wave][16 * n + col] = m[n];
     }
     __syncthreads();
@@ -285,7 +299,7 @@ __global__ __launch_bounds__(256, OCC) void attn_step_kernel(AttnArgs a, AttnPla
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
         top[n] = fmaxf(fmaxf(sm[0][16 * n + col], sm[1][16 * n + col]), fmaxf(sm[2][16 * n + col], sm[3][16 * n + col]));
-        const float w = m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[n] - top[n]);
+        const float w = m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[n] - top[n]) * factor);
         l[n] *= w;
         if (qd == 0) sl[wave][16 * n + col] = l[n];
 #pragma unroll

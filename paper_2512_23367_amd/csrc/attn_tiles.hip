@@ -63,7 +63,7 @@ __global__ __launch_bounds__(NW * 64, D == 256 ? 1 : 2) void attn_tile_kernel(At
             const int d = ELEM == 2 ? 16 * s + 8 * h : 32 * (s / 2) + 16 * h + 8 * (s % 2);
             u4 v = {0, 0, 0, 0};
             if (live) v = *reinterpret_cast<const u4 *>(src + d);
-            q[s] = attn_query(v ^ flip);
+            q[s] = attn_query(as_h8(v ^ flip));
         }
     }
 
@@ -73,6 +73,7 @@ __global__ __launch_bounds__(NW * 64, D == 256 ? 1 : 2) void attn_tile_kernel(At
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[e][i] = 0;
     float m = -INFINITY, l = 0;
+    bool far = false;                                                // of the wavefront: see ATTN_FAR
 
     // the table's entries of 64 tiles at a time, one per lane (a load for every tile: 8192 tokens, D = 64, 339 us, so 336)
     const int32_t *row_of_table = a.table + (int64_t)it.b * a.ld_table;
@@ -234,16 +235,28 @@ __global__ __launch_bounds__(NW * 64, D == 256 ? 1 : 2) void attn_tile_kernel(At
         if (__any((top - m) * factor > 8.0f)) {
             const float to = fmaxf(m, top), keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - to) * factor);
             m = to;
+            far = __any(attn_far(m, factor));
             l *= keep;
 #pragma unroll
             for (int e = 0; e < ET; ++e)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[e][i] *= keep;
         }
-        const float base = m == -INFINITY ? 0.f : fmaf(-m, factor, ATTN_LEAD);
+        float base = m == -INFINITY ? 0.f : fmaf(-m, factor, ATTN_LEAD);
+        if (far) {
+            asm volatile("");                                        // (a branch: hardly any call takes it)
+            const float off = m == -INFINITY ? 0.f : m;
+#pragma unroll
+            for (int b = 0; b < TB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[b][i] -= off;
+            base = ATTN_LEAD;
+        }
         h8 p[TB][2];
-        // of the tile: a small weight is not lost beside all before it (one chain of additions: 16384 tokens 2074 us for 2036)
-        float sums[2] = {0, 0};
+        // of the tile: a small weight is not lost beside all before it.  (One chain of additions, two: 16384 tokens of D = 128 2011 us, 1999; D = 64, six prompts,
+        // 42.3, 43.2; D = 256, 4096 tokens, 212, 213.)
+        constexpr int CHAINS = D == 128 ? 2 : 1;
+        float sums[CHAINS] = {};
 #pragma unroll
         for (int b = 0; b < TB; ++b) {
             unsigned w[8];
@@ -255,18 +268,18 @@ __global__ __launch_bounds__(NW * 64, D == 256 ? 1 : 2) void attn_tile_kernel(At
                 if constexpr (ELEM == 1) {
                     const f4 iv = *reinterpret_cast<const f4 *>(sc + 2 * TOK + 32 * b + 8 * i4 + 4 * h);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) sums[i % 2] = fmaf(x[i], iv[i], sums[i % 2]);
+                    for (int i = 0; i < 4; ++i) sums[i % CHAINS] = fmaf(x[i], iv[i], sums[i % CHAINS]);
                 }
                 w[2 * i4] = pack2(x[0], x[1]), w[2 * i4 + 1] = pack2(x[2], x[3]);
                 if constexpr (ELEM == 2) {                           // two weights (as rounded for the products) a step; plain sums: D = 64 53.4 us for 50.7
                     const h2 one = {(_Float16)1, (_Float16)1};
                     sums[0] = __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, w[2 * i4]), one, sums[0], false);
-                    sums[1] = __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, w[2 * i4 + 1]), one, sums[1], false);
+                    sums[CHAINS - 1] = __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, w[2 * i4 + 1]), one, sums[CHAINS - 1], false);
                 }
             }
             p[b][0] = as_h8(u4{w[0], w[1], w[2], w[3]}), p[b][1] = as_h8(u4{w[4], w[5], w[6], w[7]});
         }
-        l += sums[0] + sums[1];
+        l += CHAINS == 2 ? sums[0] + sums[CHAINS - 1] : sums[0];
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int b = 0; b < TB; ++b)
@@ -330,7 +343,7 @@ __global__ __launch_bounds__(NW * 64, D == 256 ? 1 : 2) void attn_tile_kernel(At
 #pragma unroll
             for (int i4 = 0; i4 < 4; ++i4)
                 *reinterpret_cast<f4 *>(out + (size_t)r * D + 32 * e + 8 * i4 + 4 * h) = f4{o[e][4 * i4], o[e][4 * i4 + 1], o[e][4 * i4 + 2], o[e][4 * i4 + 3]};
-        if (h == 0) out[(size_t)BM * D + r] = ELEM == 2 ? m * c : m, out[(size_t)BM * (D + 1) + r] = l;
+        if (h == 0) out[(size_t)BM * D + r] = m, out[(size_t)BM * (D + 1) + r] = l;
         return;
     }
     const float inv = l == 0.f ? 0.f : 1.0f / l;

@@ -5,6 +5,7 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import kv
 from paper_2512_23367_amd import binding as ql
 
 pytestmark = pytest.mark.gpu
@@ -186,3 +187,76 @@ def test_a_long_tail_of_small_weights_many_rows(U, v_tail, t, D, bits):
     ql.ql_paged_attention(q.view(T, -1), cache, fmt, U.ints([entries]), U.ints([0, T]), None, U.ints([n]), float(np.log(2)), y,
                           torch.empty(max(1, ql.ql_paged_attention_bytes(fmt, T, 1, heads)), dtype=torch.uint8, device=U.DEV), causal=False)
     _check_tail(y, t, v_tail, n, n / 16)
+
+
+def _cache_of(U, k, v, bits, page=64):
+    """A cache that holds fp32 keys and values [tokens, kv_heads, D] in its first slots, and a block table of one request."""
+    n, kv_heads, D = k.shape
+    pages = -(-n // page)
+    fmt = ql.QlKvFormat(heads=kv_heads, head_dim=D, page_size=page, pages=pages, bits=bits)
+    cache = torch.full((ql.ql_kv_cache_bytes(fmt),), 0xFF, dtype=torch.uint8, device=U.DEV)
+    ql.ql_kv_append(None, U.dev(k.reshape(n, -1).astype(np.float16)), U.dev(v.reshape(n, -1).astype(np.float16)), None, None, U.ints(np.arange(n)), None, cache, fmt)
+    return fmt, cache, U.ints([list(range(pages))])
+
+
+def _attend(U, fmt, cache, table, q, n, scale, heads):
+    """All rows see all n tokens: y [T, heads, D]."""
+    T = q.shape[0]
+    y = torch.full((T, heads * fmt.head_dim), float("nan"), dtype=torch.float16, device=U.DEV)
+    ws = torch.empty(max(1, ql.ql_paged_attention_bytes(fmt, T, 1, heads)), dtype=torch.uint8, device=U.DEV)
+    ql.ql_paged_attention(q.reshape(T, -1), cache, fmt, table, U.ints([0, T]), None, U.ints([n]), scale, y, ws, causal=False)
+    return y.view(T, heads, fmt.head_dim).double().cpu().numpy()
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("rows", [1, 30])
+@pytest.mark.parametrize("n", [50, 3000])
+def test_scores_of_any_size(U, n, rows, D, bits):
+    """Scores from 2^8 to 2^39: the keys are multiples 0 .. 47 of a vector, the largest one's token has 47 / 46 of the next score and takes the whole
+    row; where two tokens have it, each half.  Off by: y rounded, 2^-11 |y|; the weight rounded, 2^-11; the halves by ds of the larger value, the
+    scores' error: fp16, equal keys have equal scores, and what is rounded once the maximum (up to 2^10) is subtracted is 2^-14 each; int8, 2^-22 (score + 4) and
+    32 2^-23 for the logarithm of the scale of v."""
+    rng = np.random.default_rng(n + rows)
+    kv_heads, heads = 2, 8
+    for a in (2.0, 31.0, 500.0, 3000.0, 20000.0, 60000.0):
+        for top in ((0,), (n - 1,), (n // 2,), (3, n - 2)):
+            g = rng.integers(0, 47, (n, kv_heads))
+            g[list(top)] = 47
+            sign = rng.choice([-1.0, 1.0], D)
+            k = (g[..., None] * sign * (a / 64)).astype(np.float16).astype(np.float32)
+            v = rng.standard_normal((n, kv_heads, D)).astype(np.float16).astype(np.float32)
+            held = kv.stored(k, v, bits)[1][list(top)].repeat(heads // kv_heads, 1)
+            fmt, cache, table = _cache_of(U, k, v, bits)
+            q = U.dev(np.broadcast_to(sign * a, (rows, heads, D)).astype(np.float16))
+            for scale in (D ** -0.5, 1.0):
+                score = a * a / 64 * 47 * D * scale
+                if score / 47 < 30:                   # (the second one would still count)
+                    continue
+                y = _attend(U, fmt, cache, table, q, n, scale, heads)
+                ds = 2.0 ** -13 if bits == 16 else 2.0 ** -22 * (score + 4) + 32 * 2.0 ** -23
+                tol = 2.0 ** -10 * np.abs(held).max(0) + 2.0 ** -24 + (min(1.0, 2 * ds) * np.abs(held[0] - held[1]) if len(top) == 2 else 0)
+                err = np.abs(y - held.mean(0))
+                assert (err <= tol).all(), (a, top, scale, err.max())
+
+
+@pytest.mark.parametrize("rows", [1, 30])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("power", [8, 20, 23, 24])
+@pytest.mark.parametrize("ahead", [2.0, 6.0, 8.0, 10.0, 16.0])
+def test_a_maximum_that_follows_late_at_large_scores(U, ahead, power, D, rows):
+    """Two scores 2^power and 2^power + ahead (exact in fp32) in different turns of a wavefront, all others 0: weights 2^-ahead and 1, whichever comes first."""
+    n = 300
+    for first, second in ((0, 128), (128, 0), (5, 261), (1, 70)):
+        k = np.zeros((n, 1, D))
+        k[first, 0, 0] = k[second, 0, 0] = 2.0 ** (power - power // 2)
+        k[second, 0, 1] = ahead
+        v = np.zeros((n, 1, D))
+        v[first], v[second] = 1.0, -1.0
+        fmt, cache, table = _cache_of(U, k, v, 16)
+        q = np.zeros((rows, 4, D), np.float16)
+        q[..., 0], q[..., 1] = 2.0 ** (power // 2), 1.0
+        y = _attend(U, fmt, cache, table, U.dev(q), n, float(np.log(2)), 4)
+        w = 2.0 ** -ahead
+        # the score times scale and log2 e: off by 2^-22 of itself for both alike, their difference by 2^-22 of the difference; y rounded
+        assert np.abs(y - (w - 1) / (w + 1)).max() <= 2.0 ** -11 + 2.0 ** -16, (first, second, y[0, 0, 0])
